@@ -234,6 +234,9 @@ size_t carve_size(size_t& used, size_t bytes) {
   return off;
 }
 
+}  // namespace
+
+namespace epara {
 // SM count of a device (cached; 148 on a B200).  Tile widths of the weight-streaming GEMMs depend on it.
 int device_sm_count(int device) {
   static int cache[64] = {0};
@@ -245,6 +248,11 @@ int device_sm_count(int device) {
   }
   return cache[device];
 }
+
+void* tensor_map_encoder() { return reinterpret_cast<void*>(get_encode_fn()); }
+}  // namespace epara
+
+namespace {
 
 // Builds the op list of a model.  With c == nullptr only counts workspace bytes (in *need).
 // Buffers are requested through `get`, which either carves or counts.

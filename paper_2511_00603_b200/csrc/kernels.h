@@ -106,4 +106,36 @@ cudaError_t launch_attn_encoder(const AttnEncGroup* groups, int n_groups, int to
                                 cudaStream_t st);
 int attn_encoder_q_blocks(int T);
 
+int device_sm_count(int device);
+void* tensor_map_encoder();              // the driver's cuTensorMapEncodeTiled, null where there is none
+
+// 8-bit KV cache (kv8.cu): one call's arguments, passed to the kernels by value.
+struct Kv8Append {
+  const bf16* k;
+  const bf16* v;
+  unsigned char* codes;
+  float* scales;
+  const int32_t* q_rows;
+  const int32_t* kv_lens;
+  const int32_t* tables;
+  int* status;
+  long long kv_pages;
+  int k_stride, v_stride, table_stride, T, Hkv, max_q, max_len, pages_per_request;
+};
+struct Kv8Attn {
+  const bf16* q;
+  const unsigned char* codes;
+  const float* scales;
+  const int32_t* q_rows;
+  const int32_t* kv_lens;
+  const int32_t* tables;
+  bf16* out;
+  float* partial;          // [T][Hq][max_chunks][hd + 2]: maximum, sum, unnormalised output
+  int* status;
+  long long kv_pages;
+  int q_stride, table_stride, T, Hkv, G, max_q, max_len;
+  int tiles;               // row tiles of a request
+  int chunk, max_chunks;   // tokens of a chunk, chunks of the longest request
+};
+
 }  // namespace epara

@@ -24,7 +24,9 @@ MODEL_MLP, MODEL_VIT, MODEL_DECODER = 0, 1, 2
 GEMM_TCGEN05, GEMM_SIMT, GEMM_TCGEN05_UNFUSED = 0, 1, 2
 EPI_BIAS, EPI_GELU, EPI_SWIGLU, EPI_RESID_F32 = 1, 2, 4, 8
 K_NAMES = ["gather", "norm", "gemm", "rope", "attn_dec", "attn_combine", "attn_enc", "assemble", "output", "gemm_stream", "trace", "attn_prefill"]
-ERR_PAGE_APPEND, ERR_PAGE_ATTEND, ERR_SELFTEST_WAIT = 101, 102, 90
+ERR_PAGE_APPEND, ERR_PAGE_ATTEND, ERR_ROWS, ERR_SELFTEST_WAIT = 101, 102, 103, 90
+T_BF16, T_F32 = 0, 1
+GEMM_I8_MAX_K = 131071
 DECODE_STATUS_OFFSET = 192
 K_COUNT = len(K_NAMES)
 
@@ -67,13 +69,19 @@ class GemmProblem(C.Structure):
                 ("ldc", C.c_int), ("epilogue", C.c_int)]
 
 
+class GemmI8Problem(C.Structure):
+    _fields_ = [("A", C.c_void_p), ("W", C.c_void_p), ("a_scale", C.c_void_p), ("w_scale", C.c_void_p), ("C", C.c_void_p), ("bias", C.c_void_p),
+                ("M", C.c_int), ("N", C.c_int), ("K", C.c_int), ("lda", C.c_int), ("ldw", C.c_int), ("ldc", C.c_int), ("epilogue", C.c_int)]
+
+
 EXPORTS = ["epara_init", "epara_register_model", "epara_submit", "epara_submit_many", "epara_step", "epara_collect",
            "epara_step_profile", "epara_set_profile", "epara_destroy", "epara_strerror", "epara_model_workspace_bytes",
            "epara_dp_group_count", "epara_inter_request_count", "epara_admit_queue", "epara_grouped_gemm",
            "epara_gemm_scratch_bytes", "epara_gemm_scratch_bytes_for", "epara_decode_attention", "epara_decode_attention_scratch_bytes",
            "epara_decode_attention_static", "epara_static_scratch_bytes", "epara_decode_attention_static_status",
            "epara_set_max_profile_launches", "epara_selftest_bounded_wait", "epara_offload_probabilities", "epara_simulate",
-           "epara_place_sssp", "epara_gemm_plan", "epara_collect_ready"]
+           "epara_place_sssp", "epara_gemm_plan", "epara_collect_ready", "epara_rms_norm_i8", "epara_gemm_i8", "epara_kv8_append",
+           "epara_kv8_attention", "epara_kv8_attention_scratch_bytes"]
 
 lib.epara_init.argtypes = [C.POINTER(Config), C.POINTER(C.c_void_p)]
 lib.epara_register_model.argtypes = [C.c_void_p, C.POINTER(ModelDesc), C.POINTER(C.c_int)]
@@ -115,6 +123,15 @@ lib.epara_decode_attention_static.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C
 lib.epara_decode_attention_static_status.argtypes = [C.c_int, C.POINTER(C.c_int)]
 lib.epara_set_max_profile_launches.argtypes = [C.c_void_p, C.c_int]
 lib.epara_selftest_bounded_wait.argtypes = [C.c_int, C.c_void_p, C.c_ulonglong, C.c_void_p, C.POINTER(C.c_int)]
+lib.epara_rms_norm_i8.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_longlong, C.c_void_p, C.c_longlong, C.c_void_p, C.c_longlong,
+                                  C.c_void_p, C.c_float, C.c_void_p, C.c_longlong, C.c_void_p, C.c_int, C.c_int]
+lib.epara_gemm_i8.argtypes = [C.c_int, C.c_void_p, C.POINTER(GemmI8Problem), C.c_void_p]
+lib.epara_kv8_append.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_longlong, C.c_void_p,
+                                 C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p]
+lib.epara_kv8_attention.argtypes = [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_longlong, C.c_void_p, C.c_void_p, C.c_void_p,
+                                    C.c_int, C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+lib.epara_kv8_attention_scratch_bytes.argtypes = [C.c_int] * 8
+lib.epara_kv8_attention_scratch_bytes.restype = C.c_size_t
 lib.epara_static_scratch_bytes.argtypes = []
 lib.epara_static_scratch_bytes.restype = C.c_size_t
 
@@ -379,6 +396,50 @@ def epara_decode_attention_static_status(device: int = 0):
     """(status, code) of the last allocation-free decode-attention call on the device."""
     code = C.c_int(0)
     return lib.epara_decode_attention_static_status(device, C.byref(code)), code.value
+
+
+# ----------------------------------------------------------------------------- 8-bit decoder layer
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def epara_rms_norm_i8(x, gain, q, scales, stream_ptr: int, resid=None, resid_out=None, eps: float = 1e-5, device: int = 0):
+    """x [rows, d] bf16 or fp32, gain bf16 [d] or None (no norm), q int8 [rows, d], scales fp32 [rows]; resid, resid_out fp32 [rows, d] or None."""
+    _check(lib.epara_rms_norm_i8(device, stream_ptr, x.data_ptr(), T_F32 if x.dtype.itemsize == 4 else T_BF16, x.stride(0), _ptr(resid),
+                                 0 if resid is None else resid.stride(0), _ptr(resid_out), 0 if resid_out is None else resid_out.stride(0), _ptr(gain),
+                                 eps, q.data_ptr(), q.stride(0), scales.data_ptr(), x.shape[0], x.shape[1]), "epara_rms_norm_i8")
+
+
+def epara_gemm_i8(problem: Dict, stream_ptr: int, status, device: int = 0):
+    """problem: dict with torch tensors A int8 [M, lda], W int8 [N, ldw], a_scale fp32 [M], w_scale fp32 [N], C, optional bias, and M, N, K, and
+    optionally the epilogue flags under "epilogue" (or "epi"); status: int32 [1], see epara.h."""
+    p = problem
+    A, W, out = p["A"], p["W"], p["C"]
+    g = GemmI8Problem(A.data_ptr(), W.data_ptr(), p["a_scale"].data_ptr(), p["w_scale"].data_ptr(), out.data_ptr(), _ptr(p.get("bias")), p["M"], p["N"],
+                      p["K"], A.stride(0), W.stride(0), out.stride(0), p.get("epilogue", p.get("epi", 0)))
+    _check(lib.epara_gemm_i8(device, stream_ptr, g, status.data_ptr()), "epara_gemm_i8")
+
+
+def epara_kv8_append(k, v, kv8_layer, kv_scales, kv_lens, tables, max_len: int, status, stream_ptr: int, q_rows=None, max_q: int = 1, device: int = 0,
+                     kv_pages: int = 0):
+    """k, v: bf16 [T, Hkv, hd], the heads of a row next to each other; kv8_layer e4m3 [pages, 2, Hkv, 16, hd], kv_scales fp32 [pages, 2, Hkv];
+    kv_lens int32 [B] (new tokens included), tables int32 [B, stride], q_rows int32 [B + 1] or None.  kv_pages: pages the call may touch."""
+    _check(lib.epara_kv8_append(device, stream_ptr, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), kv8_layer.data_ptr(), kv_scales.data_ptr(),
+                                kv_pages or kv8_layer.shape[0], _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), kv_lens.shape[0],
+                                k.shape[0], kv8_layer.shape[2], kv8_layer.shape[4], max_q, max_len, status.data_ptr()), "epara_kv8_append")
+
+
+def epara_kv8_attention_scratch_bytes(B: int, T: int, Hq: int, Hkv: int, hd: int, max_q: int, max_len: int, device: int = 0) -> int:
+    return lib.epara_kv8_attention_scratch_bytes(device, B, T, Hq, Hkv, hd, max_q, max_len)
+
+
+def epara_kv8_attention(q, kv8_layer, kv_scales, kv_lens, tables, out, Hq: int, Hkv: int, hd: int, max_len: int, scratch, status, stream_ptr: int,
+                        q_rows=None, max_q: int = 1, device: int = 0, kv_pages: int = 0):
+    """q: bf16 [T, q_stride]; out bf16 [T, Hq * hd]; scratch: a tensor of epara_kv8_attention_scratch_bytes() bytes, or None where that is 0."""
+    _check(lib.epara_kv8_attention(device, stream_ptr, q.data_ptr(), q.stride(0), kv8_layer.data_ptr(), kv_scales.data_ptr(),
+                                   kv_pages or kv8_layer.shape[0], _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), out.data_ptr(),
+                                   kv_lens.shape[0], q.shape[0], Hq, Hkv, hd, max_q, max_len, _ptr(scratch),
+                                   0 if scratch is None else scratch.numel() * scratch.element_size(), status.data_ptr()), "epara_kv8_attention")
 
 
 def epara_selftest_bounded_wait(status_dev, stream_ptr: int, limit_ns: int = 1_000_000, device: int = 0):

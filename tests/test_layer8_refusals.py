@@ -1,0 +1,95 @@
+"""The entry points of the 8-bit decoder layer refuse what they cannot take before anything reaches a GPU."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def E():
+    from paper_2511_00603_b200 import build
+    build.build()
+    from paper_2511_00603_b200 import epara
+    return epara
+
+
+P = 1 << 20    # an address that is never read: every call below is refused on the host
+
+
+def _norm(E, **k):
+    a = dict(x=P, x_type=0, x_stride=64, resid=P, resid_stride=64, resid_out=P, resid_out_stride=64, gain=P, eps=1e-5, q=P, q_stride=64, scales=P, rows=2, d=64)
+    a.update(k)
+    return E.lib.epara_rms_norm_i8(0, None, *a.values())
+
+
+@pytest.mark.parametrize("bad", [dict(x=None), dict(q=None), dict(scales=None), dict(rows=-1), dict(d=0), dict(x_type=2), dict(x_stride=63), dict(q_stride=63),
+                                 dict(resid_stride=63), dict(resid_out_stride=1), dict(resid=None), dict(x=P + 1), dict(x_type=1, x=P + 2), dict(scales=P + 2),
+                                 dict(resid=P + 2), dict(gain=P + 1), dict(eps=-1.0), dict(eps=float("nan"))])
+def test_norm_refuses(E, bad):
+    assert _norm(E, **bad) == E.E_INVALID
+
+
+def test_empty_calls_are_fine(E):
+    assert _norm(E, rows=0) == E.OK
+    assert _gemm(E, M=0) == E.OK
+    assert _append(E, B=0, T=0) == E.OK and _append(E, T=0, q_rows=P) == E.OK
+    assert _attn(E, B=0, T=0) == E.OK
+
+
+def _gemm(E, status=P, **k):
+    a = dict(A=P, W=P, a_scale=P, w_scale=P, C=P, bias=P, M=3, N=32, K=48, lda=48, ldw=48, ldc=32, epilogue=0)
+    a.update(k)
+    return E.lib.epara_gemm_i8(0, None, E.GemmI8Problem(*a.values()), status)
+
+
+@pytest.mark.parametrize("bad", [dict(A=None), dict(W=None), dict(C=None), dict(a_scale=None), dict(w_scale=None), dict(M=-1), dict(N=0), dict(K=0), dict(lda=40, K=40),
+                                 dict(ldw=56), dict(lda=32), dict(A=P + 8), dict(W=P + 4), dict(C=P + 2), dict(a_scale=P + 4), dict(w_scale=P + 4),
+                                 dict(epilogue=1, bias=None), dict(epilogue=1, bias=P + 2), dict(epilogue=16), dict(epilogue=12), dict(epilogue=4, N=33), dict(ldc=31),
+                                 dict(epilogue=4, ldc=15), dict(status=None), dict(status=P + 2)])
+def test_gemm_refuses(E, bad):
+    assert _gemm(E, **bad) == E.E_INVALID
+
+
+def test_gemm_refuses_sums_past_31_bits(E):
+    assert _gemm(E, K=E.GEMM_I8_MAX_K + 1, lda=1 << 18, ldw=1 << 18) == E.E_UNSUPPORTED
+
+
+def _append(E, **k):
+    a = dict(k=P, k_stride=256, v=P, v_stride=256, kv8=P, scales=P, pages=10, q_rows=None, lens=P, tables=P, table_stride=4, B=2, T=2, Hkv=2, hd=128, max_q=1,
+             max_len=64, status=P)
+    a.update(k)
+    return E.lib.epara_kv8_append(0, None, *a.values())
+
+
+def _attn(E, **k):
+    a = dict(q=P, q_stride=1024, kv8=P, scales=P, pages=10, q_rows=None, lens=P, tables=P, table_stride=4, out=P, B=2, T=2, Hq=8, Hkv=2, hd=128, max_q=1, max_len=64,
+             scratch=P, scratch_bytes=1 << 30, status=P)
+    a.update(k)
+    return E.lib.epara_kv8_attention(0, None, *a.values())
+
+
+CACHE = [dict(kv8=None), dict(scales=None), dict(lens=None), dict(tables=None), dict(status=None), dict(pages=0), dict(B=-1), dict(T=-1), dict(Hkv=0), dict(hd=0),
+         dict(max_q=0), dict(max_len=0), dict(kv8=P + 8), dict(scales=P + 2), dict(q_rows=P + 2), dict(lens=P + 2), dict(tables=P + 1), dict(status=P + 2),
+         dict(table_stride=3), dict(max_q=2), dict(T=3)]
+
+
+@pytest.mark.parametrize("bad", CACHE + [dict(k=None), dict(v=None), dict(k=P + 8), dict(v=P + 2), dict(k_stride=257), dict(v_stride=252), dict(k_stride=248)])
+def test_append_refuses(E, bad):
+    assert _append(E, **bad) == E.E_INVALID
+
+
+@pytest.mark.parametrize("bad", CACHE + [dict(q=None), dict(out=None), dict(Hq=0), dict(Hq=7), dict(q=P + 8), dict(q_stride=1025), dict(q_stride=1016), dict(out=P + 1)])
+def test_attention_refuses(E, bad):
+    assert _attn(E, **bad) == E.E_INVALID
+
+
+def test_cache_calls_refuse_other_head_sizes(E):
+    assert _append(E, hd=96) == E.E_UNSUPPORTED and _attn(E, hd=32) == E.E_UNSUPPORTED
+
+
+def test_attention_asks_for_its_scratch(E):
+    need = E.epara_kv8_attention_scratch_bytes(2, 2, 8, 2, 128, 1, 4096)
+    assert need > 0
+    big = dict(max_len=4096, table_stride=256)
+    assert _attn(E, scratch_bytes=need - 1, **big) == E.E_RESOURCE
+    assert _attn(E, scratch=None, scratch_bytes=need, **big) == E.E_INVALID
+    assert _attn(E, scratch=P + 4, scratch_bytes=need, **big) == E.E_INVALID
+    assert E.epara_kv8_attention_scratch_bytes(2, 2, 8, 2, 128, 1, 64) == 0       # a single chunk needs none
+    assert E.epara_kv8_attention_scratch_bytes(2, 2, 7, 2, 128, 1, 64) == 0
