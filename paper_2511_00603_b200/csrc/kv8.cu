@@ -17,11 +17,9 @@ namespace {
 constexpr int PAGE = EPARA_KV_PAGE;
 constexpr float TINY_SCALE = 1.17549435e-38f;     // 2^-126
 
-// two fp32 -> two e4m3 codes (lo in the low byte), nearest even; what is not finite becomes e4m3's NaN
+// two fp32 -> two e4m3 codes (lo in the low byte), nearest even, NaN to NaN
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
   uint16_t r;
-  lo = fabsf(lo) <= 3.4028234e38f ? lo : __int_as_float(0x7fffffff);
-  hi = fabsf(hi) <= 3.4028234e38f ? hi : __int_as_float(0x7fffffff);
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
@@ -50,7 +48,7 @@ constexpr int APPEND_WARPS = 8;
 
 template <int HD>
 __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8Append a) {
-  constexpr int E = HD / 32;                       // values of a token in a lane
+  constexpr int LPR = HD / 8, TPL = 32 / LPR, NL = PAGE / TPL;    // lanes to a token (8 values each), tokens to a load, loads
   pdl_wait();
   const int b = blockIdx.x / a.pages_per_request, j = blockIdx.x % a.pages_per_request;
   int row, n;
@@ -65,92 +63,93 @@ __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8
   const int end = first + min(n, a.max_q);
   const int pg = first / PAGE + j;
   if (pg * PAGE >= end) return;
+  const int lane = threadIdx.x & 31, t0 = lane / LPR, c = lane % LPR;
+  const int s0 = max(first - pg * PAGE, 0), s1 = min(end - pg * PAGE, PAGE);   // the page's new slots
+  const int t = blockIdx.y * APPEND_WARPS + (threadIdx.x >> 5);
+  if (t >= 2 * a.Hkv) return;
+  const int kvh = t >> 1, is_v = t & 1, stride = is_v ? a.v_stride : a.k_stride;
+  const bf16* const src = (is_v ? a.v : a.k) + (size_t)row * stride + kvh * HD + c * 8;
   const int page = a.tables[(size_t)b * a.table_stride + pg];
+  uint4 x[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int s = i * TPL + t0;
+    x[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (s >= s0 && s < s1) x[i] = __ldcg(reinterpret_cast<const uint4*>(src + (long long)(pg * PAGE + s - first) * stride));
+  }
   if (page < 0 || page >= a.kv_pages) {
     if (threadIdx.x == 0 && blockIdx.y == 0) atomicExch(a.status, ERR_PAGE_APPEND);
     return;
   }
-  const int s0 = max(first - pg * PAGE, 0), s1 = min(end - pg * PAGE, PAGE);   // the page's new slots
-  const int lane = threadIdx.x & 31;
-  for (int t = blockIdx.y * APPEND_WARPS + (threadIdx.x >> 5); t < 2 * a.Hkv; t += gridDim.y * APPEND_WARPS) {
-    const int kvh = t >> 1, is_v = t & 1;
-    const bf16* src = is_v ? a.v + (size_t)row * a.v_stride : a.k + (size_t)row * a.k_stride;
-    const int stride = is_v ? a.v_stride : a.k_stride;
-    src += (long long)(pg * PAGE - first) * stride + kvh * HD + lane * E;
-    uint32_t x[PAGE][E / 2];
+  float* const sp = a.scales + ((size_t)page * 2 + is_v) * a.Hkv + kvh;
+  const float was = s0 > 0 ? *sp : 0.f;            // (a page that starts afresh had none)
+  uint2* const code = reinterpret_cast<uint2*>(a.codes + (((size_t)page * 2 + is_v) * a.Hkv + kvh) * PAGE * HD) + lane;   // [i * 32]: this lane's 8 of token i * TPL + t0
+  // largest magnitude, as bf16 bits (which order like the values); from 0x7f80 on it is no number
+  uint32_t m2 = 0;
 #pragma unroll
-    for (int s = 0; s < PAGE; ++s) {
-      const bool is_new = s >= s0 && s < s1;
-      if (E == 4) {
-        uint2 u = make_uint2(0u, 0u);
-        if (is_new) u = __ldcg(reinterpret_cast<const uint2*>(src + (long long)s * stride));
-        x[s][0] = u.x; x[s][E / 2 - 1] = u.y;
-      } else {
-        x[s][0] = is_new ? __ldcg(reinterpret_cast<const uint32_t*>(src + (long long)s * stride)) : 0u;
-      }
-    }
-    // largest finite magnitude, as bf16 bits (which order like the values)
-    uint32_t top = 0;
+  for (int i = 0; i < NL; ++i)
+    m2 = __vmaxu2(m2, __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu)));
+  uint32_t top = __reduce_max_sync(0xffffffffu, max(m2 & 0xffffu, m2 >> 16));
+  if (top >= 0x7f80u) {                            // infinities become NaN, and neither counts for the maximum
+    top = 0;
+    auto drop = [&](uint32_t& w) {
+      const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
+      if (lo >= 0x7f80u) w = (w & 0xffff0000u) | 0x7fffu; else top = max(top, lo);
+      if (hi >= 0x7f80u) w = (w & 0xffffu) | 0x7fff0000u; else top = max(top, hi);
+    };
 #pragma unroll
-    for (int s = 0; s < PAGE; ++s)
-#pragma unroll
-      for (int e = 0; e < E / 2; ++e) {
-        const uint32_t lo = x[s][e] & 0x7fffu, hi = (x[s][e] >> 16) & 0x7fffu;
-        top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-      }
+    for (int i = 0; i < NL; ++i) { drop(x[i].x); drop(x[i].y); drop(x[i].z); drop(x[i].w); }
     top = __reduce_max_sync(0xffffffffu, top);
-    // 448 = 1.75 x 2^8: the smallest power of two that brings top = 1.m x 2^e to 448 is 2^(e-8) up to m = .75, else 2^(e-7)
-    const int ex = (int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
-    float scale = ex >= 1 ? __int_as_float(ex << 23) : TINY_SCALE;
-    float* const sp = a.scales + ((size_t)page * 2 + is_v) * a.Hkv + kvh;
-    uint32_t* const code = reinterpret_cast<uint32_t*>(a.codes + (((size_t)page * 2 + is_v) * a.Hkv + kvh) * PAGE * HD);
-    if (s0 > 0) {
-      const float was = *sp;
-      if (was >= scale) {
-        scale = was;
-      } else {
-        const float f = was / scale;
-        for (int s = 0; s < s0; ++s) {
-          if (E == 4) {
-            uint32_t* c = code + s * 32 + lane;
-            const uint32_t o = *c;
-            const float2 l = to_float2(o), h = to_float2(o >> 16);
-            *c = to_e4m3x2(l.x * f, l.y * f) | to_e4m3x2(h.x * f, h.y * f) << 16;
-          } else {
-            uint16_t* c = reinterpret_cast<uint16_t*>(code) + s * 32 + lane;
-            const float2 l = to_float2(*c);
-            *c = (uint16_t)to_e4m3x2(l.x * f, l.y * f);
-          }
-        }
-      }
-    }
-    __syncwarp();                                  // every lane has read the old scale
-    if (lane == 0) *sp = scale;
-    const bool pow2 = (__float_as_uint(scale) & 0x007fffffu) == 0;
-    const float inv = 1.f / scale;                 // exact for a power of two; a caller's other scales are divided by
-    auto put = [&](float v) { return pow2 ? v * inv : __fdiv_rn(v, scale); };
+  }
+  // 448 = 1.75 x 2^8: the smallest power of two that brings top = 1.m x 2^e to 448 is 2^(e-8) up to m = .75, else 2^(e-7)
+  const int ex = (int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
+  float scale = ex >= 1 ? __int_as_float(ex << 23) : TINY_SCALE;
+  if (s0 > 0) {
+    if (was >= scale) {
+      scale = was;
+    } else {
+      const float f = was / scale;
+      uint2 o[NL];
 #pragma unroll
-    for (int s = 0; s < PAGE; ++s) {
-      if (s < s0 || s >= s1) continue;
-      const uint32_t lo = to_e4m3x2(put(__uint_as_float(x[s][0] << 16)), put(__uint_as_float(x[s][0] & 0xffff0000u)));
-      if (E == 4) {
-        const uint32_t hi = to_e4m3x2(put(__uint_as_float(x[s][E / 2 - 1] << 16)), put(__uint_as_float(x[s][E / 2 - 1] & 0xffff0000u)));
-        code[s * 32 + lane] = lo | hi << 16;
-      } else {
-        reinterpret_cast<uint16_t*>(code)[s * 32 + lane] = (uint16_t)lo;
-      }
+      for (int i = 0; i < NL; ++i) if (i * TPL + t0 < s0) o[i] = code[i * 32];
+      auto again = [&](uint32_t w) {
+        const float2 l = to_float2(w), h = to_float2(w >> 16);
+        return to_e4m3x2(l.x * f, l.y * f) | to_e4m3x2(h.x * f, h.y * f) << 16;
+      };
+#pragma unroll
+      for (int i = 0; i < NL; ++i) if (i * TPL + t0 < s0) code[i * 32] = make_uint2(again(o[i].x), again(o[i].y));
     }
+  }
+  __syncwarp();                                    // every lane has read the old scale
+  if (lane == 0) *sp = scale;
+  auto store = [&](auto put) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int s = i * TPL + t0;
+      if (s < s0 || s >= s1) continue;
+      auto four = [&](uint32_t u, uint32_t v) {
+        return to_e4m3x2(put(__uint_as_float(u << 16)), put(__uint_as_float(u & 0xffff0000u))) |
+               to_e4m3x2(put(__uint_as_float(v << 16)), put(__uint_as_float(v & 0xffff0000u))) << 16;
+      };
+      code[i * 32] = make_uint2(four(x[i].x, x[i].y), four(x[i].z, x[i].w));
+    }
+  };
+  if ((__float_as_uint(scale) & 0x007fffffu) == 0) {              // a power of two: its reciprocal is exact
+    const float inv = 1.f / scale;
+    store([&](float v) { return v * inv; });
+  } else {                                         // somebody else's scale
+    store([&](float v) { return __fdiv_rn(v, scale); });
   }
 }
 
 // ------------------------------------------------------------------------------------------------ attention, few rows
-// A block takes a chunk of a request's tokens for one kv head and a tile of 16 query rows (row = new token x query head of the
+// A block takes a chunk of a request's tokens for one kv head and a tile of 8 NT query rows (row = new token x query head of the
 // kv head's group); its four warps take the chunk's pages in turn, with the pages of a ring of their own in flight (16-byte
 // asynchronous copies), and are merged at the end.  The products run on mma.sync m16n8k16 in fp16, which holds every e4m3 code
-// exactly: S = Q K^T with the query rows as M, O += P V.  Scales stay out of the matrices: a page's K scale multiplies its
-// scores, its V scale the probabilities, relative to the largest V scale so far so that fp16 holds them.  Which token an
-// MMA column or k index stands for is free as long as both sides agree, and is chosen so that a lane reads 16 consecutive
-// bytes of K and of V and no value moves between lanes.
+// exactly, with the query rows as the 8 columns: S^T = K Q^T (16 tokens x 8 rows), O^T += V^T P^T (16 dims x 8 rows).  Scales stay
+// out of the matrices: a page's K scale multiplies its scores, its V scale the probabilities, relative to the largest V scale
+// so far so that fp16 holds them.  Which dim a k index of the first product stands for, and which one a row of the second, is
+// free, and is chosen so that a lane reads 16 consecutive bytes of K and of V.
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -167,44 +166,54 @@ __device__ __forceinline__ uint2 lds8(uint32_t a) {
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
   return v;
 }
-__device__ __forceinline__ void mma_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t u) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(u));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
 __device__ __forceinline__ uint32_t u4(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
 
-// Byte offset of 16-byte piece p of token r in a staged tile; placed so that the reads of a quarter warp fall into different banks.
+// Byte offset of 16-byte piece p of token r in a staged tile; placed so that the reads of a quarter warp (hd 64, V: of half a warp)
+// fall into different banks.
 template <int HD>
 __device__ __forceinline__ int k_piece(int r, int p) {
   return HD == 128 ? r * 128 + ((p ^ ((r & 1) << 2)) << 4) : r * 64 + (p << 4);
 }
 template <int HD>
 __device__ __forceinline__ int v_piece(int r, int p) {
-  return HD == 128 ? r * 128 + ((p ^ (((r >> 2) & 3) << 1)) << 4)
-                   : (r >> 1) * 128 + ((((r & 1) ^ ((r >> 2) & 1)) << 6) | ((p ^ (((r >> 3) & 1) << 1)) << 4));
+  return HD == 128 ? r * 128 + ((p ^ (((r >> 1) & 3) << 1)) << 4)
+                   : (r >> 1) * 128 + ((((r & 1) ^ ((r >> 1) & 1)) << 6) | ((p ^ (((r >> 2) & 1) << 1)) << 4));
 }
 
 constexpr int KV8_WARPS = 4;
-constexpr int KV8_STAGES = 4;
+template <int HD, int NT>
+struct Kv8Geo {
+  static constexpr int STAGES = HD == 128 && NT == 1 ? 3 : 4, BLOCKS = NT == 1 ? 4 : 3;     // pages in a warp's ring, blocks to an SM
+  static constexpr int RING = KV8_WARPS * STAGES * 2 * PAGE * HD, MERGE = KV8_WARPS * 8 * NT * HD * 4, SMEM = RING > MERGE ? RING : MERGE;
+};
 
-template <int HD>
-constexpr int kv8_smem() {
-  return std::max(KV8_WARPS * KV8_STAGES * 2 * PAGE * HD, KV8_WARPS * 16 * HD * 4);
-}
-
-template <int HD>
-__global__ void __launch_bounds__(KV8_WARPS * 32, 3) kv8_attn_kernel(const Kv8Attn a) {
+template <int HD, int NT>
+__global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_attn_kernel(const Kv8Attn a) {
   constexpr float LOG2E = 1.4426950408889634f;
-  constexpr int KK = HD / 64, NT = HD / 8;         // 64-wide pieces of a row; n tiles of O
-  constexpr int TILE = PAGE * HD;
+  constexpr int KK = HD / 64, MT = HD / 16;        // 64-wide pieces of a row; m tiles of O^T
+  constexpr int TILE = PAGE * HD, ST = Kv8Geo<HD, NT>::STAGES, TR = 8 * NT;
   extern __shared__ __align__(128) unsigned char ring[];
-  __shared__ float sm_m[KV8_WARPS][16], sm_l[KV8_WARPS][16];
+  __shared__ float sm_m[KV8_WARPS][TR], sm_l[KV8_WARPS][TR];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
   const int b = blockIdx.x / a.tiles, tile = blockIdx.x % a.tiles, kvh = blockIdx.y, chunk = blockIdx.z;
   pdl_wait();
@@ -216,20 +225,22 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, 3) kv8_attn_kernel(const Kv8At
     if (threadIdx.x == 0 && tile == 0 && kvh == 0 && chunk == 0) atomicExch(a.status, ERR_ROWS);
     n = a.max_q;
   }
-  const int rows = min(n * G - tile * 16, 16);     // of this tile
+  const int rows = min(n * G - tile * TR, TR);     // of this tile
   if (rows <= 0) return;
-  const int seen_top = seen0 + (tile * 16 + rows - 1) / G;
+  const int seen_top = seen0 + (tile * TR + rows - 1) / G;
   const int t_begin = chunk * a.chunk, t_end = min(seen_top, t_begin + a.chunk);
   if (t_begin >= t_end) return;
-  int seen[2];                                     // of this thread's rows gq and gq + 8
+  int seen[NT][2];                                 // tokens seen by this thread's rows 8 y + 2 tq + {0, 1}
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int r = gq + 8 * e;
-    seen[e] = r < rows ? seen0 + (tile * 16 + r) / G : 0;
-  }
-  const int seen_least = seen0 + tile * 16 / G;    // pages up to here are whole for every row
+  for (int y = 0; y < NT; ++y)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = 8 * y + 2 * tq + e;
+      seen[y][e] = r < rows ? seen0 + (tile * TR + r) / G : 0;
+    }
+  const int seen_least = min(seen0 + tile * TR / G, t_end);        // pages up to here are whole for every row
 
-  // ---- the pages of this warp: lanes hold the ids and scales of 32 of them, and of the 32 after those
+  // ---- the pages of this warp: lanes hold the ids and scales of 32 of them, and of the 32 after those (by parity)
   const int32_t* const table = a.tables + (size_t)b * a.table_stride;
   const int pg0 = t_begin / PAGE + warp, pg_end = (t_end + PAGE - 1) / PAGE;
   const int n_pages = pg0 < pg_end ? (pg_end - pg0 + KV8_WARPS - 1) / KV8_WARPS : 0;
@@ -250,40 +261,42 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, 3) kv8_attn_kernel(const Kv8At
     }
     return s;
   };
-  int id_cur = load_id(0), id_next = load_id(1);
-  const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(ring) + warp * KV8_STAGES * 2 * TILE;
+  int id_even = load_id(0), id_odd = load_id(1);
+  const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(ring) + warp * ST * 2 * TILE;
+  uint32_t k_dst[TILE / 512], v_dst[TILE / 512];
+#pragma unroll
+  for (int x = 0; x < TILE / 512; ++x) {
+    const int piece = x * 32 + lane, r = piece / (HD / 16), p = piece % (HD / 16);
+    k_dst[x] = k_piece<HD>(r, p);
+    v_dst[x] = TILE + v_piece<HD>(r, p);
+  }
+  int fill = 0;                                    // stage of the next page to request
   auto issue = [&](int i) {                        // page i of this warp into its stage (one commit group each, empty ones too)
     if (i < n_pages) {
-      const int id = __shfl_sync(0xffffffffu, (i & 32) == 0 ? id_cur : id_next, i & 31);
+      const int id = __shfl_sync(0xffffffffu, (i & 32) == 0 ? id_even : id_odd, i & 31);
       if (id >= 0) {
-        const uint32_t dst = my_ring + (i % KV8_STAGES) * 2 * TILE;
-        const unsigned char* k = a.codes + ((size_t)id * 2 * a.Hkv + kvh) * TILE;
+        const uint32_t dst = my_ring + fill * 2 * TILE;
+        const unsigned char* k = a.codes + ((size_t)id * 2 * a.Hkv + kvh) * TILE + lane * 16;
         const unsigned char* v = k + (size_t)a.Hkv * TILE;
 #pragma unroll
-        for (int x = 0; x < TILE / 512; ++x) {
-          const int piece = x * 32 + lane, r = piece / (HD / 16), p = piece % (HD / 16);
-          cp16(dst + k_piece<HD>(r, p), k + piece * 16);
-        }
+        for (int x = 0; x < TILE / 512; ++x) cp16(dst + k_dst[x], k + x * 512);
 #pragma unroll
-        for (int x = 0; x < TILE / 512; ++x) {
-          const int piece = x * 32 + lane, r = piece / (HD / 16), p = piece % (HD / 16);
-          cp16(dst + TILE + v_piece<HD>(r, p), v + piece * 16);
-        }
+        for (int x = 0; x < TILE / 512; ++x) cp16(dst + v_dst[x], v + x * 512);
       }
     }
     cp_commit();
+    if (++fill == ST) fill = 0;
   };
-  // (ids by position: batch x is in id_cur or id_next by the parity of x, see the end of the loop)
 #pragma unroll
-  for (int i = 0; i < KV8_STAGES - 1; ++i) issue(i);
-  float2 sc_cur = load_scales(id_cur), sc_next = load_scales(id_next);
+  for (int i = 0; i < ST - 1; ++i) issue(i);
+  float2 sc_even = load_scales(id_even), sc_odd = load_scales(id_odd);
 
-  // ---- Q: fp16, a row's largest value brought to [2^14, 2^15) by a power of two that joins the score's factor
-  uint32_t q[KK * 4][4];
-  float row_f[2];
+  // ---- Q as the B operand, fp16: a row's largest value is brought to [2^14, 2^15) by a power of two that joins the score's factor
+  uint32_t q[NT][KK * 4][2];
+  float row_f[NT][2];
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int r = gq + 8 * e, rr = tile * 16 + r;
+  for (int y = 0; y < NT; ++y) {
+    const int r = 8 * y + gq, rr = tile * TR + r;
     uint4 u[KK][2];
     float top = 0.f;
 #pragma unroll
@@ -296,161 +309,181 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, 3) kv8_attn_kernel(const Kv8At
         float f[8];
         unpack8(u[kk][x], f);
 #pragma unroll
-        for (int y = 0; y < 8; ++y) top = fmaxf(top, fabsf(f[y]));
+        for (int z = 0; z < 8; ++z) top = fmaxf(top, fabsf(f[z]));
       }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const int ex = min(max((int)(__float_as_uint(top) >> 23), 15), 254);     // biased exponent
-    const float up = __uint_as_float((uint32_t)(254 + 14 - ex < 254 ? 254 + 14 - ex : 254) << 23);   // 2^(14 - (ex - 127))
-    row_f[e] = LOG2E * rsqrtf((float)HD) / up;
+    const float up = __uint_as_float((uint32_t)min(254 + 14 - ex, 254) << 23);                      // 2^(14 - (ex - 127))
+    const float f = LOG2E * rsqrtf((float)HD) / up;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) row_f[y][e] = __shfl_sync(0xffffffffu, f, (2 * tq + e) * 4);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        float f[8];
-        unpack8(u[kk][x], f);
+        float v[8];
+        unpack8(u[kk][x], v);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {              // MMA kk * 4 + 2 x + j takes elements 4 j .. 4 j + 3
-          q[kk * 4 + 2 * x + j][e] = pack_f16(f[4 * j] * up, f[4 * j + 1] * up);
-          q[kk * 4 + 2 * x + j][2 + e] = pack_f16(f[4 * j + 2] * up, f[4 * j + 3] * up);
+          q[y][kk * 4 + 2 * x + j][0] = pack_f16(v[4 * j] * up, v[4 * j + 1] * up);
+          q[y][kk * 4 + 2 * x + j][1] = pack_f16(v[4 * j + 2] * up, v[4 * j + 3] * up);
         }
       }
   }
 
-  float o[NT][4];
+  float o[NT][MT][4];
+  float m[NT][2], l[NT][2], v_ref = TINY_SCALE, inv_ref = 1.f / TINY_SCALE;
 #pragma unroll
-  for (int j = 0; j < NT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, v_ref = TINY_SCALE;
+  for (int y = 0; y < NT; ++y) {
+    m[y][0] = m[y][1] = -INFINITY;
+    l[y][0] = l[y][1] = 0.f;
+#pragma unroll
+    for (int j = 0; j < MT; ++j) o[y][j][0] = o[y][j][1] = o[y][j][2] = o[y][j][3] = 0.f;
+  }
 
+  int stage = 0;
   for (int i = 0; i < n_pages; ++i) {
     if ((i & 31) == 0) {
-      if (i > 0) {                                 // the next 32 pages
-        if (i & 32) { id_cur = load_id(i / 32 + 1); sc_cur = load_scales(id_cur); }
-        else { id_next = load_id(i / 32 + 1); sc_next = load_scales(id_next); }
+      if (i > 0) {                                 // the 32 pages after the next ones
+        if (i & 32) { id_even = load_id(i / 32 + 1); sc_even = load_scales(id_even); }
+        else { id_odd = load_id(i / 32 + 1); sc_odd = load_scales(id_odd); }
       }
-      float top = (i & 32) == 0 ? sc_cur.y : sc_next.y;
+      float top = (i & 32) == 0 ? sc_even.y : sc_odd.y;
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
       if (top > v_ref) {
         const float f = v_ref / top;
 #pragma unroll
-        for (int j = 0; j < NT; ++j) { o[j][0] *= f; o[j][1] *= f; o[j][2] *= f; o[j][3] *= f; }
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+          for (int j = 0; j < MT; ++j) { o[y][j][0] *= f; o[y][j][1] *= f; o[y][j][2] *= f; o[y][j][3] *= f; }
         v_ref = top;
+        inv_ref = 1.f / top;
       }
     }
-    const int id = __shfl_sync(0xffffffffu, (i & 32) == 0 ? id_cur : id_next, i & 31);
-    const float ks = __shfl_sync(0xffffffffu, (i & 32) == 0 ? sc_cur.x : sc_next.x, i & 31);
-    const float vs = __shfl_sync(0xffffffffu, (i & 32) == 0 ? sc_cur.y : sc_next.y, i & 31);
-    issue(i + KV8_STAGES - 1);                     // into the stage that the page before this one has left
-    cp_wait<KV8_STAGES - 1>();
+    const int id = __shfl_sync(0xffffffffu, (i & 32) == 0 ? id_even : id_odd, i & 31);
+    const float ks = __shfl_sync(0xffffffffu, (i & 32) == 0 ? sc_even.x : sc_odd.x, i & 31);
+    const float vf = __shfl_sync(0xffffffffu, (i & 32) == 0 ? sc_even.y : sc_odd.y, i & 31) * inv_ref;
+    issue(i + ST - 1);                             // into the stage that the page before this one has left
+    cp_wait<ST - 1>();
     __syncwarp();
+    const uint32_t kt = my_ring + stage * 2 * TILE, vt = kt + TILE;
+    if (++stage == ST) stage = 0;
     if (id >= 0) {
-      const uint32_t kt = my_ring + (i % KV8_STAGES) * 2 * TILE, vt = kt + TILE;
       const int t0 = (pg0 + i * KV8_WARPS) * PAGE;
-      float s[2][4];
+      // S^T: rows gq and gq + 8 are tokens t0 + gq and t0 + gq + 8, columns 2 tq + {0, 1} query rows
+      float s[NT][4];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
-        const int r = 4 * (gq >> 1) + 2 * x + (gq & 1);            // token of column gq of n tile x
+      for (int y = 0; y < NT; ++y) s[y][0] = s[y][1] = s[y][2] = s[y][3] = 0.f;
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          const uint4 u = lds16(kt + k_piece<HD>(r, kk * 4 + tq));
+      for (int kk = 0; kk < KK; ++kk) {
+        const uint4 lo = lds16(kt + k_piece<HD>(gq, kk * 4 + tq)), hi = lds16(kt + k_piece<HD>(gq + 8, kk * 4 + tq));
 #pragma unroll
-          for (int j = 0; j < 4; ++j) mma_f16(s[x], q[kk * 4 + j], to_f16x2(u4(u, j)), to_f16x2(u4(u, j) >> 16));
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t a0 = to_f16x2(u4(lo, j)), a1 = to_f16x2(u4(hi, j)), a2 = to_f16x2(u4(lo, j) >> 16), a3 = to_f16x2(u4(hi, j) >> 16);
+#pragma unroll
+          for (int y = 0; y < NT; ++y) mma_f16(s[y], a0, a1, a2, a3, q[y][kk * 4 + j][0], q[y][kk * 4 + j][1]);
         }
       }
-      // scores to the log2 domain, masked; a thread has tokens t0 + 4 tq + 2 x + {0, 1} of rows gq and gq + 8
-      const float f0 = row_f[0] * ks, f1 = row_f[1] * ks;
-      const bool whole = t0 + PAGE <= min(seen_least, t_end);
+      const bool whole = t0 + PAGE <= seen_least;
+      bool raise = false;
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          s[x][c] *= c < 2 ? f0 : f1;
-          if (!whole && t0 + 4 * tq + 2 * x + (c & 1) >= seen[c >> 1]) s[x][c] = -INFINITY;
-        }
-      // the running maximum is only raised when a score passes it by more than 2^8
-      const float top0 = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[1][0], s[1][1]));
-      const float top1 = fmaxf(fmaxf(s[0][2], s[0][3]), fmaxf(s[1][2], s[1][3]));
-      if (__any_sync(0xffffffffu, top0 > m[0] + 8.f || top1 > m[1] + 8.f)) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float top = e ? top1 : top0;
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          if (top > m[e]) {
-            const float f = exp2f(m[e] - top);
-            m[e] = top;
-            l[e] *= f;
-#pragma unroll
-            for (int j = 0; j < NT; ++j) { o[j][2 * e] *= f; o[j][2 * e + 1] *= f; }
-          }
-        }
+      for (int y = 0; y < NT; ++y) {
+        const float f0 = row_f[y][0] * ks, f1 = row_f[y][1] * ks;
+        s[y][0] *= f0; s[y][1] *= f1; s[y][2] *= f0; s[y][3] *= f1;          // to the log2 domain
       }
-      const float m0 = m[0] == -INFINITY ? 0.f : m[0], m1 = m[1] == -INFINITY ? 0.f : m[1];
-      const float vf = vs / v_ref;
-      uint32_t p[4];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float p0 = exp2f(s[x][0] - m0), p1 = exp2f(s[x][1] - m0), p2 = exp2f(s[x][2] - m1), p3 = exp2f(s[x][3] - m1);
-        l[0] += p0 + p1;
-        l[1] += p2 + p3;
-        p[2 * x] = pack_f16(p0 * vf, p1 * vf);
-        p[2 * x + 1] = pack_f16(p2 * vf, p3 * vf);
-      }
-      // V: bytes of two tokens interleaved, then two codes at a time to fp16; k index 2 tq + {0, 1} and + 8 stand for
-      // tokens 4 tq + {0, 1} and + 2, column gq of n tile j for dim gq * NT + j
-      uint32_t w[4][HD / 32];
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        if constexpr (HD == 128) {
-          const uint4 u = lds16(vt + v_piece<HD>(4 * tq + y, gq));
-          w[y][0] = u.x; w[y][1] = u.y; w[y][2] = u.z; w[y][3] = u.w;
-        } else {
-          const uint2 u = lds8(vt + v_piece<HD>(4 * tq + y, gq >> 1) + (gq & 1) * 8);
-          w[y][0] = u.x; w[y][1] = u.y;
-        }
-      }
-      bool odd = false;                            // NaN codes that not every row sees
       if (!whole) {
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const int t = t0 + 4 * tq + y;
-          if (t >= t_end) {                        // slots behind the last token may hold anything
+        for (int y = 0; y < NT; ++y)
 #pragma unroll
-            for (int z = 0; z < HD / 32; ++z) w[y][z] = 0u;
+          for (int c = 0; c < 4; ++c) if (t0 + gq + 8 * (c >> 1) >= seen[y][c & 1]) s[y][c] = -INFINITY;
+      }
+      // the running maximum is only raised when a score passes it by more than 2^8
+#pragma unroll
+      for (int y = 0; y < NT; ++y) raise |= fmaxf(s[y][0], s[y][2]) > m[y][0] + 8.f || fmaxf(s[y][1], s[y][3]) > m[y][1] + 8.f;
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int y = 0; y < NT; ++y)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float top = fmaxf(s[y][e], s[y][2 + e]);
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            if (top > m[y][e]) {
+              const float f = ex2(m[y][e] - top);
+              m[y][e] = top;
+              l[y][e] *= f;
+#pragma unroll
+              for (int j = 0; j < MT; ++j) { o[y][j][e] *= f; o[y][j][2 + e] *= f; }
+            }
           }
+      }
+      uint32_t p[NT][2];                           // P^T as the B operand
 #pragma unroll
-          for (int z = 0; z < HD / 32; ++z) odd |= __vcmpeq4(w[y][z] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0u;
+      for (int y = 0; y < NT; ++y) {
+        const float m0 = m[y][0] == -INFINITY ? 0.f : m[y][0], m1 = m[y][1] == -INFINITY ? 0.f : m[y][1];
+        const float p0 = ex2(s[y][0] - m0), p1 = ex2(s[y][1] - m1), p2 = ex2(s[y][2] - m0), p3 = ex2(s[y][3] - m1);
+        l[y][0] += p0 + p2;
+        l[y][1] += p1 + p3;
+        p[y][0] = transpose_8x8(pack_f16(p0 * vf, p1 * vf));
+        p[y][1] = transpose_8x8(pack_f16(p2 * vf, p3 * vf));
+      }
+      // V^T as the A operand: bytes of two tokens interleaved, then two codes at a time to fp16; k indices 2 tq + {0, 1} and + 8 are
+      // those tokens, rows gq and gq + 8 of m tile j the dims gq HD / 8 + 2 j + {0, 1}
+      uint32_t w[4][HD / 32];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int t = 2 * tq + (x & 1) + 8 * (x >> 1);
+        if constexpr (HD == 128) {
+          const uint4 u = lds16(vt + v_piece<HD>(t, gq));
+          w[x][0] = u.x; w[x][1] = u.y; w[x][2] = u.z; w[x][3] = u.w;
+        } else {
+          const uint2 u = lds8(vt + v_piece<HD>(t, gq >> 1) + (gq & 1) * 8);
+          w[x][0] = u.x; w[x][1] = u.y;
         }
       }
-      if (__any_sync(0xffffffffu, odd)) {
-        // a zero probability times NaN would be NaN: NaN codes are taken out and the rows that do see one get it here, by a
-        // product of 0/1 matrices
-        uint32_t see[4];
+      if (!whole) {
+        bool odd = false;                          // NaN codes that not every row sees
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 4; ++x) {
+          if (t0 + 2 * tq + (x & 1) + 8 * (x >> 1) >= t_end) {     // slots behind the last token may hold anything
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
-            see[2 * x + e] = (t0 + 4 * tq + 2 * x < seen[e] ? 0x3c00u : 0u) | (t0 + 4 * tq + 2 * x + 1 < seen[e] ? 0x3c000000u : 0u);
-#pragma unroll
-        for (int z = 0; z < HD / 32; ++z) {
-          uint32_t bad[4];
-#pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const uint32_t mask = __vcmpeq4(w[y][z] & 0x7f7f7f7fu, 0x7f7f7f7fu);
-            bad[y] = mask & 0x38383838u;           // e4m3 1.0
-            w[y][z] &= ~mask;
+            for (int z = 0; z < HD / 32; ++z) w[x][z] = 0u;
           }
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t a0 = __byte_perm(bad[0], bad[1], h ? 0x7362 : 0x5140), a1 = __byte_perm(bad[2], bad[3], h ? 0x7362 : 0x5140);
+          for (int z = 0; z < HD / 32; ++z) odd |= __vcmpeq4(w[x][z] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0u;
+        }
+        if (__any_sync(0xffffffffu, odd)) {
+          // a zero probability times NaN would be NaN: NaN codes are taken out, and the rows that do see one get it from a product
+          // of 0/1 matrices
+          uint32_t see[NT][2];
 #pragma unroll
-            for (int y = 0; y < 2; ++y) {
-              float c[4] = {0.f, 0.f, 0.f, 0.f};
-              mma_f16(c, see, to_f16x2(a0 >> (16 * y)), to_f16x2(a1 >> (16 * y)));
+          for (int y = 0; y < NT; ++y)
 #pragma unroll
-              for (int d = 0; d < 4; ++d) if (c[d] > 0.f) o[z * 4 + h * 2 + y][d] = nan_f();
+            for (int x = 0; x < 2; ++x) {
+              const int t = t0 + gq + 8 * x;
+              see[y][x] = transpose_8x8((t < seen[y][0] ? 0x3c00u : 0u) | (t < seen[y][1] ? 0x3c000000u : 0u));
+            }
+#pragma unroll
+          for (int z = 0; z < HD / 32; ++z) {
+            uint32_t bad[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t mask = __vcmpeq4(w[x][z] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+              bad[x] = mask & 0x38383838u;         // e4m3 1.0
+              w[x][z] &= ~mask;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t b0 = __byte_perm(bad[0], bad[1], h ? 0x7362 : 0x5140), b1 = __byte_perm(bad[2], bad[3], h ? 0x7362 : 0x5140);
+#pragma unroll
+              for (int y = 0; y < NT; ++y) {
+                float c[4] = {0.f, 0.f, 0.f, 0.f};
+                mma_f16(c, to_f16x2(b0), to_f16x2(b0 >> 16), to_f16x2(b1), to_f16x2(b1 >> 16), see[y][0], see[y][1]);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) if (c[d] > 0.f) o[y][2 * z + h][d] = nan_f();
+              }
             }
           }
         }
@@ -459,35 +492,38 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, 3) kv8_attn_kernel(const Kv8At
       for (int z = 0; z < HD / 32; ++z)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint32_t a0 = __byte_perm(w[0][z], w[1][z], h ? 0x7362 : 0x5140), a1 = __byte_perm(w[2][z], w[3][z], h ? 0x7362 : 0x5140);
-          mma_f16(o[z * 4 + h * 2], p, to_f16x2(a0), to_f16x2(a1));
-          mma_f16(o[z * 4 + h * 2 + 1], p, to_f16x2(a0 >> 16), to_f16x2(a1 >> 16));
+          const uint32_t b0 = __byte_perm(w[0][z], w[1][z], h ? 0x7362 : 0x5140), b1 = __byte_perm(w[2][z], w[3][z], h ? 0x7362 : 0x5140);
+          const uint32_t a0 = to_f16x2(b0), a1 = to_f16x2(b0 >> 16), a2 = to_f16x2(b1), a3 = to_f16x2(b1 >> 16);
+#pragma unroll
+          for (int y = 0; y < NT; ++y) mma_f16(o[y][2 * z + h], a0, a1, a2, a3, p[y][0], p[y][1]);
         }
     }
     __syncwarp();                                  // the stage may be filled again
   }
 
-  // ---- merge of the four warps, in warp order; thread: one row, a run of dims
+  // ---- merge of the four warps, in warp order; thread: one row, two dims at a time
   cp_wait<0>();
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    l[e] += __shfl_xor_sync(0xffffffffu, l[e], 1);
-    l[e] += __shfl_xor_sync(0xffffffffu, l[e], 2);
-  }
+  for (int y = 0; y < NT; ++y)
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int x = 4; x < 32; x <<= 1) l[y][e] += __shfl_xor_sync(0xffffffffu, l[y][e], x);
   __syncthreads();
   float* const sm_o = reinterpret_cast<float*>(ring);              // [warp][row][dim]
 #pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int r = gq + 8 * e;
-    if (tq == 0) { sm_m[warp][r] = m[e]; sm_l[warp][r] = l[e]; }
+  for (int y = 0; y < NT; ++y)
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+    for (int e = 0; e < 2; ++e) {
+      const int r = 8 * y + 2 * tq + e;
+      if (gq == 0) { sm_m[warp][r] = m[y][e]; sm_l[warp][r] = l[y][e]; }
 #pragma unroll
-      for (int j = 0; j < NT; ++j) sm_o[(warp * 16 + r) * HD + (2 * tq + c) * NT + j] = o[j][2 * e + c] * v_ref;
-  }
+      for (int j = 0; j < MT; ++j)
+        *reinterpret_cast<float2*>(sm_o + (warp * TR + r) * HD + gq * (HD / 8) + 2 * j) = make_float2(o[y][j][e] * v_ref, o[y][j][2 + e] * v_ref);
+    }
   __syncthreads();
   for (int idx = threadIdx.x; idx < rows * (HD / 2); idx += KV8_WARPS * 32) {
-    const int r = idx / (HD / 2), d = idx % (HD / 2) * 2, rr = tile * 16 + r;
+    const int r = idx / (HD / 2), d = idx % (HD / 2) * 2, rr = tile * TR + r;
     const int sees = seen0 + rr / G;
     if (sees <= t_begin) continue;
     float mm = sm_m[0][r];
@@ -496,12 +532,12 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, 3) kv8_attn_kernel(const Kv8At
     float ll = 0.f, ox = 0.f, oy = 0.f;
 #pragma unroll
     for (int w = 0; w < KV8_WARPS; ++w) {
-      const float f = sm_m[w][r] == -INFINITY ? 0.f : exp2f(sm_m[w][r] - mm);
-      const float2 ow = *reinterpret_cast<const float2*>(sm_o + (w * 16 + r) * HD + d);
+      // (a warp without a maximum has seen no token of this row, or nothing but NaN)
+      const float f = sm_m[w][r] == -INFINITY ? 1.f : ex2(sm_m[w][r] - mm);
+      const float2 ow = *reinterpret_cast<const float2*>(sm_o + (w * TR + r) * HD + d);
       ll += sm_l[w][r] * f;
-      // (a warp without a token of this row has zeros, or what other rows' products left: not its business)
-      ox += sm_m[w][r] == -INFINITY && sm_l[w][r] == 0.f ? 0.f : ow.x * f;
-      oy += sm_m[w][r] == -INFINITY && sm_l[w][r] == 0.f ? 0.f : ow.y * f;
+      ox += ow.x * f;
+      oy += ow.y * f;
     }
     const size_t qr = (size_t)(row0 + rr / G) * a.Hkv * G + kvh * G + rr % G;
     if (sees <= a.chunk) {
@@ -600,20 +636,23 @@ int kv8_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) {
   return (int)std::min(std::min(std::max((c + 63) / 64 * 64, 64ll), 1024ll), whole);
 }
 
-struct AttnPlan { int tiles, chunk, chunks; };
+struct AttnPlan { int nt, tiles, chunk, chunks; };
 AttnPlan attn_plan(int B, int Hq, int Hkv, int max_q, int max_len, int sm_count) {
   AttnPlan p;
-  p.tiles = (int)(((long long)max_q * (Hq / Hkv) + 15) / 16);
+  const long long rows = (long long)max_q * (Hq / Hkv);
+  p.nt = rows <= 8 ? 1 : 2;
+  p.tiles = (int)((rows + 8 * p.nt - 1) / (8 * p.nt));
   p.chunk = kv8_chunk(B, p.tiles, Hkv, max_len, sm_count);
   p.chunks = (max_len + p.chunk - 1) / p.chunk;
   return p;
 }
 
-template <int HD>
+template <int HD, int NT>
 cudaError_t launch_attn(const Kv8Attn& a, int B, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(kv8_attn_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kv8_smem<HD>());
+  const auto kernel = kv8_attn_kernel<HD, NT>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Kv8Geo<HD, NT>::SMEM);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kv8_attn_kernel<HD>, dim3((unsigned)(B * a.tiles), (unsigned)a.Hkv, (unsigned)a.max_chunks), dim3(KV8_WARPS * 32), kv8_smem<HD>(), st, a);
+  e = launch_pdl(kernel, dim3((unsigned)(B * a.tiles), (unsigned)a.Hkv, (unsigned)a.max_chunks), dim3(KV8_WARPS * 32), Kv8Geo<HD, NT>::SMEM, st, a);
   if (e != cudaSuccess || a.max_chunks == 1) return e;
   return launch_pdl(kv8_merge_kernel<HD>, dim3((unsigned)(B * a.max_q), (unsigned)(a.Hkv * a.G)), dim3(MERGE_WARPS * 32), 0, st, a);
 }
@@ -687,7 +726,8 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
   a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
   if ((long long)B * a.tiles > 0x7fffffffll || (long long)B * a.max_q > 0x7fffffffll || a.max_chunks > 65535) return EPARA_E_UNSUPPORTED;
   if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;
-  const cudaError_t e = hd == 128 ? launch_attn<128>(a, B, (cudaStream_t)cuda_stream) : launch_attn<64>(a, B, (cudaStream_t)cuda_stream);
+  const cudaError_t e = hd == 128 ? (p.nt == 1 ? launch_attn<128, 1>(a, B, (cudaStream_t)cuda_stream) : launch_attn<128, 2>(a, B, (cudaStream_t)cuda_stream))
+                                  : (p.nt == 1 ? launch_attn<64, 1>(a, B, (cudaStream_t)cuda_stream) : launch_attn<64, 2>(a, B, (cudaStream_t)cuda_stream));
   return e == cudaSuccess ? EPARA_OK : EPARA_E_CUDA;
 }
 
