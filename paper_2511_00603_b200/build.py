@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libepara.so")
 SOURCES = ["epara_api.cu", "kernels_misc.cu", "gemm_simt.cu", "gemm_tc.cu", "gemm_stream.cu", "gemm_swap.cu", "attention.cu", "attention_flash.cu", "policy.cu",
-           "selftest.cu", "norm_i8.cu", "gemm_i8.cu", "kv8.cu"]
+           "selftest.cu", "norm_i8.cu", "gemm_i8.cu", "kv8.cu", "kv8_flash.cu"]
 # Python side of epara_collect; the file's name carries the interpreter's ABI, another interpreter does not load it
 FAST_SRC, FAST_LIB = os.path.join(CSRC, "fastcall.cpp"), os.path.join(HERE, "_fastcall" + sysconfig.get_config_var("EXT_SUFFIX"))
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC"]

@@ -133,9 +133,11 @@ struct Kv8Attn {
   float* partial;          // [T][Hq][max_chunks][hd + 2]: maximum, sum, unnormalised output
   int* status;
   long long kv_pages;
-  int q_stride, table_stride, T, Hkv, G, max_q, max_len;
+  int q_stride, table_stride, B, T, Hkv, G, max_q, max_len;
   int tiles;               // row tiles of a request
   int chunk, max_chunks;   // tokens of a chunk, chunks of the longest request
 };
+constexpr int KV8_FLASH_ROWS = 256;      // query rows of a CTA in the kernel for many rows (kv8_flash.cu)
+cudaError_t launch_kv8_flash(const Kv8Attn& a, int hd, cudaStream_t st);
 
 }  // namespace epara

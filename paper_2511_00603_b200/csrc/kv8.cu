@@ -9,37 +9,13 @@
 #include "../../include/epara.h"
 #include "common.cuh"
 #include "kernels.h"
+#include "kv8.cuh"
 
 namespace epara {
 
 namespace {
 
 constexpr int PAGE = EPARA_KV_PAGE;
-constexpr float TINY_SCALE = 1.17549435e-38f;     // 2^-126
-
-// two fp32 -> two e4m3 codes (lo in the low byte), nearest even, NaN to NaN
-__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-// two codes (the low 16 bits) -> two fp16, exact
-__device__ __forceinline__ uint32_t to_f16x2(uint32_t two_codes) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two_codes));
-  return r;
-}
-__device__ __forceinline__ float2 to_float2(uint32_t two_codes) {
-  const uint32_t h = to_f16x2(two_codes);
-  return __half22float2(*reinterpret_cast<const __half2*>(&h));
-}
-
-// A request's new rows [row, row + n), from the prefix sums `q_rows` (or one row each); what they say is clamped to the T rows.
-__device__ __forceinline__ void new_rows(const int32_t* q_rows, int b, int T, int& row, int& n) {
-  if (q_rows == nullptr) { row = b; n = b < T ? 1 : 0; return; }
-  row = min(max(q_rows[b], 0), T);
-  n = min(max(q_rows[b + 1], row), T) - row;
-}
 
 // ------------------------------------------------------------------------------------------------ append
 // A block takes one page of one request, a warp one (K or V, kv head) of it: 16 x hd values in registers, so the maximum, the
@@ -103,7 +79,7 @@ __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8
   }
   // 448 = 1.75 x 2^8: the smallest power of two that brings top = 1.m x 2^e to 448 is 2^(e-8) up to m = .75, else 2^(e-7)
   const int ex = (int)(top >> 7) - 8 + ((top & 0x7fu) > 0x60u ? 1 : 0);
-  float scale = ex >= 1 ? __int_as_float(ex << 23) : TINY_SCALE;
+  float scale = ex >= 1 ? __int_as_float(ex << 23) : KV8_TINY_SCALE;
   if (s0 > 0) {
     if (was >= scale) {
       scale = was;
@@ -171,19 +147,10 @@ __device__ __forceinline__ void mma_f16(float* c, uint32_t a0, uint32_t a1, uint
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  const __half2 h = __floats2half2_rn(lo, hi);
-  return *reinterpret_cast<const uint32_t*>(&h);
-}
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t u) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(u));
   return r;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
 }
 __device__ __forceinline__ uint32_t u4(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
@@ -209,7 +176,6 @@ struct Kv8Geo {
 
 template <int HD, int NT>
 __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_attn_kernel(const Kv8Attn a) {
-  constexpr float LOG2E = 1.4426950408889634f;
   constexpr int KK = HD / 64, MT = HD / 16;        // 64-wide pieces of a row; m tiles of O^T
   constexpr int TILE = PAGE * HD, ST = Kv8Geo<HD, NT>::STAGES, TR = 8 * NT;
   extern __shared__ __align__(128) unsigned char ring[];
@@ -291,7 +257,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   for (int i = 0; i < ST - 1; ++i) issue(i);
   float2 sc_even = load_scales(id_even), sc_odd = load_scales(id_odd);
 
-  // ---- Q as the B operand, fp16: a row's largest value is brought to [2^14, 2^15) by a power of two that joins the score's factor
+  // ---- Q as the B operand, fp16
   uint32_t q[NT][KK * 4][2];
   float row_f[NT][2];
 #pragma unroll
@@ -313,9 +279,8 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
       }
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int ex = min(max((int)(__float_as_uint(top) >> 23), 15), 254);     // biased exponent
-    const float up = __uint_as_float((uint32_t)min(254 + 14 - ex, 254) << 23);                      // 2^(14 - (ex - 127))
-    const float f = LOG2E * rsqrtf((float)HD) / up;
+    float up;
+    const float f = row_factor<HD>(top, up);
 #pragma unroll
     for (int e = 0; e < 2; ++e) row_f[y][e] = __shfl_sync(0xffffffffu, f, (2 * tq + e) * 4);
 #pragma unroll
@@ -333,7 +298,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   }
 
   float o[NT][MT][4];
-  float m[NT][2], l[NT][2], v_ref = TINY_SCALE, inv_ref = 1.f / TINY_SCALE;
+  float m[NT][2], l[NT][2], v_ref = KV8_TINY_SCALE, inv_ref = 1.f / KV8_TINY_SCALE;
 #pragma unroll
   for (int y = 0; y < NT; ++y) {
     m[y][0] = m[y][1] = -INFINITY;
@@ -636,25 +601,47 @@ int kv8_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) {
   return (int)std::min(std::min(std::max((c + 63) / 64 * 64, 64ll), 1024ll), whole);
 }
 
-struct AttnPlan { int nt, tiles, chunk, chunks; };
+// ... of the kernel for many rows: one CTA to an SM; a chunk of at least 512 tokens, so that what a CTA does around its loop stays small.
+int kv8_flash_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) {
+  const long long items = B * tiles * Hkv, whole = ((long long)max_len + 63) / 64 * 64;
+  if (items >= sm_count) return (int)std::min<long long>(whole, 1 << 30);
+  const long long c = ((long long)max_len * items + 2 * sm_count - 1) / (2 * sm_count);
+  return (int)std::min(std::max((c + 63) / 64 * 64, 512ll), whole);
+}
+
+struct AttnPlan { int nt, tiles, chunk, chunks; };      // nt 0: the kernel for many rows
 AttnPlan attn_plan(int B, int Hq, int Hkv, int max_q, int max_len, int sm_count) {
   AttnPlan p;
   const long long rows = (long long)max_q * (Hq / Hkv);
-  p.nt = rows <= 8 ? 1 : 2;
-  p.tiles = (int)((rows + 8 * p.nt - 1) / (8 * p.nt));
-  p.chunk = kv8_chunk(B, p.tiles, Hkv, max_len, sm_count);
+  p.nt = rows <= 8 ? 1 : rows <= 32 ? 2 : 0;
+  const int tile = p.nt ? 8 * p.nt : KV8_FLASH_ROWS;
+  p.tiles = (int)((rows + tile - 1) / tile);
+  p.chunk = p.nt ? kv8_chunk(B, p.tiles, Hkv, max_len, sm_count) : kv8_flash_chunk(B, p.tiles, Hkv, max_len, sm_count);
   p.chunks = (max_len + p.chunk - 1) / p.chunk;
   return p;
 }
 
+template <int HD>
+cudaError_t launch_merge(const Kv8Attn& a, cudaStream_t st) {
+  if (a.max_chunks == 1) return cudaSuccess;
+  return launch_pdl(kv8_merge_kernel<HD>, dim3((unsigned)(a.B * a.max_q), (unsigned)(a.Hkv * a.G)), dim3(MERGE_WARPS * 32), 0, st, a);
+}
+
 template <int HD, int NT>
-cudaError_t launch_attn(const Kv8Attn& a, int B, cudaStream_t st) {
+cudaError_t launch_attn(const Kv8Attn& a, cudaStream_t st) {
   const auto kernel = kv8_attn_kernel<HD, NT>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Kv8Geo<HD, NT>::SMEM);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kernel, dim3((unsigned)(B * a.tiles), (unsigned)a.Hkv, (unsigned)a.max_chunks), dim3(KV8_WARPS * 32), Kv8Geo<HD, NT>::SMEM, st, a);
-  if (e != cudaSuccess || a.max_chunks == 1) return e;
-  return launch_pdl(kv8_merge_kernel<HD>, dim3((unsigned)(B * a.max_q), (unsigned)(a.Hkv * a.G)), dim3(MERGE_WARPS * 32), 0, st, a);
+  e = launch_pdl(kernel, dim3((unsigned)(a.B * a.tiles), (unsigned)a.Hkv, (unsigned)a.max_chunks), dim3(KV8_WARPS * 32), Kv8Geo<HD, NT>::SMEM, st, a);
+  return e == cudaSuccess ? launch_merge<HD>(a, st) : e;
+}
+
+template <int HD>
+cudaError_t launch_attn(const Kv8Attn& a, int nt, cudaStream_t st) {
+  if (nt == 1) return launch_attn<HD, 1>(a, st);
+  if (nt == 2) return launch_attn<HD, 2>(a, st);
+  const cudaError_t e = launch_kv8_flash(a, HD, st);
+  return e == cudaSuccess ? launch_merge<HD>(a, st) : e;
 }
 
 inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
@@ -721,13 +708,12 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
   Kv8Attn a;
   a.q = (const bf16*)q; a.codes = (const unsigned char*)kv8_layer; a.scales = kv_scales; a.q_rows = q_rows; a.kv_lens = kv_lens; a.tables = tables;
   a.out = (bf16*)out; a.partial = (float*)scratch; a.status = status; a.kv_pages = kv_pages;
-  a.q_stride = q_stride; a.table_stride = table_stride; a.T = T; a.Hkv = Hkv; a.G = Hq / Hkv; a.max_q = std::min(max_q, T); a.max_len = max_len;
+  a.q_stride = q_stride; a.table_stride = table_stride; a.B = B; a.T = T; a.Hkv = Hkv; a.G = Hq / Hkv; a.max_q = std::min(max_q, T); a.max_len = max_len;
   const AttnPlan p = attn_plan(B, Hq, Hkv, a.max_q, max_len, device_sm_count(device));
   a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
-  if ((long long)B * a.tiles > 0x7fffffffll || (long long)B * a.max_q > 0x7fffffffll || a.max_chunks > 65535) return EPARA_E_UNSUPPORTED;
+  if ((long long)B * a.tiles * Hkv > 0x7fffffffll || (long long)B * a.max_q > 0x7fffffffll || a.max_chunks > 65535) return EPARA_E_UNSUPPORTED;
   if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;
-  const cudaError_t e = hd == 128 ? (p.nt == 1 ? launch_attn<128, 1>(a, B, (cudaStream_t)cuda_stream) : launch_attn<128, 2>(a, B, (cudaStream_t)cuda_stream))
-                                  : (p.nt == 1 ? launch_attn<64, 1>(a, B, (cudaStream_t)cuda_stream) : launch_attn<64, 2>(a, B, (cudaStream_t)cuda_stream));
+  const cudaError_t e = hd == 128 ? launch_attn<128>(a, p.nt, (cudaStream_t)cuda_stream) : launch_attn<64>(a, p.nt, (cudaStream_t)cuda_stream);
   return e == cudaSuccess ? EPARA_OK : EPARA_E_CUDA;
 }
 

@@ -1,0 +1,53 @@
+// Device helpers of the 8-bit cache's kernels.
+#pragma once
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace epara {
+
+constexpr float KV8_TINY_SCALE = 1.17549435e-38f;     // 2^-126
+
+// two fp32 -> two e4m3 codes (lo in the low byte), nearest even, NaN to NaN
+__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// two codes (the low 16 bits) -> two fp16, exact
+__device__ __forceinline__ uint32_t to_f16x2(uint32_t two_codes) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)two_codes));
+  return r;
+}
+__device__ __forceinline__ float2 to_float2(uint32_t two_codes) {
+  const uint32_t h = to_f16x2(two_codes);
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// A request's new rows [row, row + n), from the prefix sums `q_rows` (or one row each); what they say is clamped to the T rows.
+__device__ __forceinline__ void new_rows(const int32_t* q_rows, int b, int T, int& row, int& n) {
+  if (q_rows == nullptr) { row = b; n = b < T ? 1 : 0; return; }
+  row = min(max(q_rows[b], 0), T);
+  n = min(max(q_rows[b + 1], row), T) - row;
+}
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// A query row with the largest magnitude `top` is multiplied by `up`, a power of two that brings it to [2^14, 2^15), before it becomes
+// fp16: what is 2^-28 of the largest is still a normal number.  Returns the factor that turns the row's scores into log2 units.
+template <int HD>
+__device__ __forceinline__ float row_factor(float top, float& up) {
+  const int ex = min(max((int)(__float_as_uint(top) >> 23), 15), 254);       // biased exponent
+  up = __uint_as_float((uint32_t)min(254 + 14 - ex, 254) << 23);
+  return 1.4426950408889634f * rsqrtf((float)HD) / up;
+}
+
+}  // namespace epara

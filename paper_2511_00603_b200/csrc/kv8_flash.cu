@@ -1,0 +1,490 @@
+// Attention of many new tokens over the 8-bit cache on the sm_100a tensor cores: prompt chunks, head size 64 or 128.
+//
+// A CTA takes 256 query rows of a (request, kv head) -- row = new token x query head of the group -- as two tiles of 128, and a chunk
+// of the request's keys in steps of 64 (four pages).  Everything the MMAs read is fp16, which holds an e4m3 code exactly: K and V codes
+// are converted once per CTA, Q has its rows brought to [2^14, 2^15) by powers of two.  K's page scales multiply the scores, V's scales,
+// relative to the largest of the chunk, are folded into the converted values.  Roles:
+//   warps 0-3, 4-7  softmax of tile 0 and 1, one thread per query row (at first: that row of Q into shared memory).  A row of S is read
+//                   from tensor memory once and P written over it in fp16.  The running maximum is raised, and O rescaled, only when
+//                   it grows by more than 2^8;
+//   warp 8          issues S_g = Q_g K^T (M 128, N 64) into one of two buffers per tile;
+//   warps 9, 10     issue O_g += P_g V, P as the A operand from tensor memory, V as an MN-major B operand;
+//   warps 11-14     load a page of each step (the next step's while this one's is converted) and write it as the 128-byte-swizzled tiles
+//                   that the MMAs want.  NaN codes of V are taken out (a zero probability times NaN is NaN) and the first key
+//                   that has one is kept per dim: a row that sees it gets its NaN at the end.
+// With several chunks of keys partial results go to scratch, as in the kernel for few rows, and are merged by the same kernel.
+// Every mbarrier wait is bounded.
+#include <climits>
+
+#include "../../include/epara.h"
+#include "common.cuh"
+#include "kernels.h"
+#include "kv8.cuh"
+#include "tcgen05.cuh"
+
+namespace epara {
+
+namespace {
+
+using namespace tc;
+
+constexpr int KF_STEP = 64, KF_TILE = 128;
+constexpr int KF_S_WARP = 8, KF_PV_WARP = 9, KF_CONV_WARP = 11, KF_CONV_WARPS = 4;
+constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
+constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
+constexpr float KF_RAISE = 8.0f;
+
+template <int HD>
+struct KfGeo {
+  static constexpr int NH = HD / 64;
+  static constexpr int Q_BYTES = KF_Q_HALF * NH, KV_BYTES = KF_KV_HALF * NH;   // a tile of Q; a step's K or V
+  static constexpr int STAGES = HD == 64 ? 6 : 4;
+  static constexpr int OFF_KV = 2 * Q_BYTES;
+  static constexpr int OFF_NAN = OFF_KV + STAGES * 2 * KV_BYTES;               // first key with a NaN in V, per dim
+  static constexpr int OFF_BAR = OFF_NAN + HD * 4;
+  static constexpr int SMEM = 1024 + OFF_BAR + 512;
+  static_assert(SMEM <= 227 * 1024 && 2 * SMEM > 227 * 1024, "one CTA, which takes all of the tensor memory, to an SM");
+};
+constexpr int KF_S_COL = 0, KF_O_COL = 256;          // TMEM columns: S / P buffers 0, 1 of tile 0, of tile 1; O_0, O_1
+
+enum { KB_Q = 0, KB_S_FULL, KB_P_READY = KB_S_FULL + 4, KB_PV_DONE = KB_P_READY + 4, KB_K_FULL = KB_PV_DONE + 4, KB_K_EMPTY = KB_K_FULL + 6, KB_V_FULL = KB_K_EMPTY + 6,
+       KB_V_EMPTY = KB_V_FULL + 6, KB_COUNT = KB_V_EMPTY + 6 };
+static_assert(8 * KB_COUNT + 32 <= 512, "barrier area");
+
+__device__ __forceinline__ uint32_t kf_idesc(int n) { return (1u << 4) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24); }   // fp16 x fp16 -> fp32
+__device__ __forceinline__ uint64_t kf_desc_v(uint32_t addr) {
+  uint64_t d = make_smem_desc(addr);
+  d &= ~((uint64_t)0x3fff << 16);
+  return d | (uint64_t)(KF_KV_HALF >> 4) << 16;       // 64-dim halves
+}
+__device__ __forceinline__ void kf_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|q, 0xffffffff;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+      ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void kf_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void kf_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void un_f2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float kf_max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn a) {
+  using Geo = KfGeo<HD>;
+  constexpr int ST = Geo::STAGES, NX = HD / 32;       // ... 16-byte pieces of a page tile in a lane
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  unsigned char* const base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  int* const nan_key = reinterpret_cast<int*>(base_ptr + Geo::OFF_NAN);
+  const uint32_t bars = base + Geo::OFF_BAR;
+  auto bar = [&](int i) { return bars + 8u * i; };
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + Geo::OFF_BAR + 8 * KB_COUNT);
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* const any_nan = reinterpret_cast<int*>(tmem_slot + 2);
+  float* const v_tops = reinterpret_cast<float*>(tmem_slot + 3);      // [KF_CONV_WARPS]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // ---- the work item; the longest ones, a request's last rows, come first
+  const int bk = blockIdx.x % (a.B * a.Hkv), pair = a.tiles - 1 - blockIdx.x / (a.B * a.Hkv), b = bk / a.Hkv, kvh = bk % a.Hkv, chunk = blockIdx.y;
+  pdl_wait();
+  int row0, n;
+  new_rows(a.q_rows, b, a.T, row0, n);
+  const int G = a.G, len = min(max(a.kv_lens[b], 0), a.max_len);
+  const int seen0 = len - n + 1;                      // keys that new token 0 attends to
+  if (n > a.max_q) {
+    if (threadIdx.x == 0 && pair == 0 && kvh == 0 && chunk == 0) atomicExch(a.status, ERR_ROWS);
+    n = a.max_q;
+  }
+  const int r_first = pair * 2 * KF_TILE, rows = min(n * G - r_first, 2 * KF_TILE);
+  if (rows <= 0) return;
+  const int t_begin = chunk * a.chunk, t_end = min(seen0 + (r_first + rows - 1) / G, t_begin + a.chunk);
+  if (t_begin >= t_end) return;
+  const int n_mt = rows > KF_TILE ? 2 : 1, steps = (t_end - t_begin + KF_STEP - 1) / KF_STEP;
+  const int pg0 = t_begin / EPARA_KV_PAGE, n_pages = (t_end - t_begin + EPARA_KV_PAGE - 1) / EPARA_KV_PAGE;
+  const int32_t* const table = a.tables + (size_t)b * a.table_stride + pg0;
+  auto page_id = [&](int i) {                         // of the chunk's page i; -1: none, or outside the pool
+    int id = i < n_pages ? table[i] : -1;
+    return id < a.kv_pages ? id : -1;
+  };
+
+  if (threadIdx.x == 0) {
+    mbar_init(bar(KB_Q), 8);
+    for (int i = 0; i < 4; ++i) { mbar_init(bar(KB_S_FULL + i), 1); mbar_init(bar(KB_P_READY + i), 4); mbar_init(bar(KB_PV_DONE + i), 1); }
+    for (int s = 0; s < ST; ++s) {
+      mbar_init(bar(KB_K_FULL + s), KF_CONV_WARPS); mbar_init(bar(KB_K_EMPTY + s), 1);
+      mbar_init(bar(KB_V_FULL + s), KF_CONV_WARPS); mbar_init(bar(KB_V_EMPTY + s), n_mt);
+    }
+    *abort_flag = 0;
+    *any_nan = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = threadIdx.x; i < HD; i += KF_THREADS) nan_key[i] = INT_MAX;
+  if (warp == KF_S_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp >= KF_CONV_WARP) {
+    // the largest V scale of the chunk; ids outside the pool are reported here
+    float top = 0.f;
+    for (int i = threadIdx.x - KF_CONV_WARP * 32; i < n_pages; i += KF_CONV_WARPS * 32) {
+      const int id = page_id(i);
+      if (id >= 0) top = fmaxf(top, a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh]);
+      else atomicExch(a.status, ERR_PAGE_ATTEND);
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+    if (lane == 0) v_tops[warp - KF_CONV_WARP] = top;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  float v_ref = KV8_TINY_SCALE;
+#pragma unroll
+  for (int i = 0; i < KF_CONV_WARPS; ++i) v_ref = fmaxf(v_ref, v_tops[i]);
+
+  bool ok = true;
+  float m_ref = 0.f, l = 0.f, row_f = 0.f;            // softmax threads: the row's maximum (log2 domain), sum, score factor
+  const int g = warp >> 2, row = (warp & 3) * 32 + lane, rr = r_first + g * KF_TILE + row;         // (warps 0 .. 7)
+  const bool row_live = warp < 8 && g * KF_TILE + row < rows;
+  const int seen = row_live ? seen0 + rr / G : 0;     // keys that the row attends to
+
+  if (warp >= KF_CONV_WARP) {
+    // ------------------------------------------------------------------ converters
+    const int cw = warp - KF_CONV_WARP;               // this warp's page of a step
+    uint4 kx[NX], vx[NX];
+    int id_cur = page_id(lane * 4 + cw), id_next = page_id((lane + 32) * 4 + cw);      // of 32 steps each
+    auto scale_of = [&](int id) { return id >= 0 ? a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh] : 0.f; };
+    float vs_cur = scale_of(id_cur), vs_next = scale_of(id_next);
+    int where[NX], place[NX];                         // of a piece in the page tile and in the converted tile (its first half)
+#pragma unroll
+    for (int x = 0; x < NX; ++x) {
+      const int half = HD == 128 ? x & 1 : 0, r = (HD == 128 ? x >> 1 : x) * 8 + (lane >> 2), R = cw * 16 + r;
+      where[x] = r * HD + half * 64 + (lane & 3) * 16;
+      place[x] = half * KF_KV_HALF + R * 128 + ((((lane & 3) * 2) ^ (R & 7)) << 4);
+    }
+    auto load = [&](int j, int is_v, uint4* u) {
+      const int id = __shfl_sync(0xffffffffu, (j & 32) == 0 ? id_cur : id_next, j & 31);
+#pragma unroll
+      for (int x = 0; x < NX; ++x) u[x] = make_uint4(0u, 0u, 0u, 0u);
+      if (j < steps && id >= 0) {
+        const unsigned char* p = a.codes + (((size_t)id * 2 + is_v) * a.Hkv + kvh) * EPARA_KV_PAGE * HD;
+#pragma unroll
+        for (int x = 0; x < NX; ++x) u[x] = __ldg(reinterpret_cast<const uint4*>(p + where[x]));
+      }
+    };
+    auto put = [&](unsigned char* tile, int x, const uint4& u, bool scaled, uint32_t f) {
+      uint4 lo = make_uint4(to_f16x2(u.x), to_f16x2(u.x >> 16), to_f16x2(u.y), to_f16x2(u.y >> 16));
+      uint4 hi = make_uint4(to_f16x2(u.z), to_f16x2(u.z >> 16), to_f16x2(u.w), to_f16x2(u.w >> 16));
+      if (scaled) {
+        lo.x = hmul2(lo.x, f); lo.y = hmul2(lo.y, f); lo.z = hmul2(lo.z, f); lo.w = hmul2(lo.w, f);
+        hi.x = hmul2(hi.x, f); hi.y = hmul2(hi.y, f); hi.z = hmul2(hi.z, f); hi.w = hmul2(hi.w, f);
+      }
+      *reinterpret_cast<uint4*>(tile + place[x]) = lo;
+      *reinterpret_cast<uint4*>(tile + (place[x] ^ 16)) = hi;
+    };
+    load(0, 0, kx);
+    load(0, 1, vx);
+    for (int j = 0; j < steps; ++j) {
+      const int slot = j % ST;
+      const uint32_t parity = ((j / ST) & 1u) ^ 1u;
+      if ((j & 31) == 0 && j > 0) {                   // the 32 steps after the next ones
+        const int id = page_id((lane + j + 32) * 4 + cw);
+        if (j & 32) { id_cur = id; vs_cur = scale_of(id); } else { id_next = id; vs_next = scale_of(id); }
+      }
+      unsigned char* const kt = base_ptr + Geo::OFF_KV + slot * 2 * Geo::KV_BYTES;
+      if (j >= ST && !mbar_wait(bar(KB_K_EMPTY + slot), parity, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 23); break; }
+#pragma unroll
+      for (int x = 0; x < NX; ++x) put(kt, x, kx[x], false, 0u);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(KB_K_FULL + slot));
+      load(j + 1, 0, kx);
+      const float vs = __shfl_sync(0xffffffffu, (j & 32) == 0 ? vs_cur : vs_next, j & 31);
+      const uint32_t vf = pack_f16(vs / v_ref, vs / v_ref);
+      const int t0 = t_begin + j * KF_STEP + cw * 16;
+      uint32_t nan = 0;
+#pragma unroll
+      for (int x = 0; x < NX; ++x) {
+        if (t0 + 16 > t_end && t0 + (HD == 128 ? x >> 1 : x) * 8 + (lane >> 2) >= t_end) vx[x] = make_uint4(0u, 0u, 0u, 0u);   // may hold anything
+        // (a byte of 0x7f, sign aside, carries into its top bit)
+        nan |= ((vx[x].x & 0x7f7f7f7fu) + 0x01010101u) | ((vx[x].y & 0x7f7f7f7fu) + 0x01010101u) | ((vx[x].z & 0x7f7f7f7fu) + 0x01010101u) |
+               ((vx[x].w & 0x7f7f7f7fu) + 0x01010101u);
+      }
+      if (nan & 0x80808080u) {
+        *any_nan = 1;
+#pragma unroll
+        for (int x = 0; x < NX; ++x) {
+          const int key = t0 + (HD == 128 ? x >> 1 : x) * 8 + (lane >> 2), dim = (HD == 128 ? x & 1 : 0) * 64 + (lane & 3) * 16;
+          auto clean = [&](uint32_t& w, int d) {
+            const uint32_t mask = __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu);
+            w &= ~mask;
+            for (int e = 0; e < 4; ++e) if (mask >> (8 * e) & 1u) atomicMin(nan_key + d + e, key);
+          };
+          clean(vx[x].x, dim); clean(vx[x].y, dim + 4); clean(vx[x].z, dim + 8); clean(vx[x].w, dim + 12);
+        }
+      }
+      __syncwarp();
+      if (j >= ST && !mbar_wait(bar(KB_V_EMPTY + slot), parity, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 24); break; }
+#pragma unroll
+      for (int x = 0; x < NX; ++x) put(kt + Geo::KV_BYTES, x, vx[x], true, vf);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(KB_V_FULL + slot));
+      load(j + 1, 1, vx);
+    }
+    if (!ok) *abort_flag = 1;
+  } else if (warp == KF_S_WARP) {
+    // ------------------------------------------------------------------ issuer of S
+    const uint32_t idesc = kf_idesc(KF_STEP);
+    if (!mbar_wait<false>(bar(KB_Q), 0u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 25); }
+    for (int j = 0; j < steps && ok; ++j) {
+      const int slot = j % ST, sb = j & 1;
+      if (!mbar_wait<false>(bar(KB_K_FULL + slot), (j / ST) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 26); break; }
+      const uint64_t dk = make_smem_desc(base + Geo::OFF_KV + slot * 2 * Geo::KV_BYTES);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (t >= n_mt) break;
+        // the buffer holds P until the P V of two steps ago is complete
+        if (j >= 2 && !mbar_wait<false>(bar(KB_PV_DONE + 2 * t + sb), ((j >> 1) - 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 27); break; }
+        tc_fence_after();
+        const uint64_t dq = make_smem_desc(base + t * Geo::Q_BYTES);
+        const uint32_t d = tmem_base + KF_S_COL + t * 128 + sb * 64;
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k)
+          mma_f16_elect(d, dq + (uint64_t)((k >> 2) * (KF_Q_HALF >> 4) + (k & 3) * 2), dk + (uint64_t)((k >> 2) * (KF_KV_HALF >> 4) + (k & 3) * 2), idesc, k > 0 ? 1u : 0u);
+        mma_commit_elect(bar(KB_S_FULL + 2 * t + sb));
+      }
+      if (!ok) break;
+      mma_commit_elect(bar(KB_K_EMPTY + slot));
+    }
+    if (!ok) *abort_flag = 1;
+  } else if (warp >= KF_PV_WARP) {
+    // ------------------------------------------------------------------ issuers of O_t += P_t V
+    const int t = warp - KF_PV_WARP;
+    const uint32_t idesc = kf_idesc(HD) | (1u << 16), d = tmem_base + KF_O_COL + t * HD;           // B operand MN-major
+    for (int j = 0; j < steps && t < n_mt; ++j) {
+      const int slot = j % ST, sb = j & 1;
+      if (!mbar_wait<false>(bar(KB_V_FULL + slot), (j / ST) & 1u, abort_flag) || !mbar_wait<false>(bar(KB_P_READY + 2 * t + sb), (j >> 1) & 1u, abort_flag)) {
+        ok = false;
+        if (lane == 0) atomicExch(a.status, 28);
+        break;
+      }
+      tc_fence_after();
+      const uint32_t p = tmem_base + KF_S_COL + t * 128 + sb * 64;
+      const uint64_t dv = kf_desc_v(base + Geo::OFF_KV + slot * 2 * Geo::KV_BYTES + Geo::KV_BYTES);
+#pragma unroll
+      for (int k = 0; k < KF_STEP / 16; ++k) kf_mma_ts(d, p + k * 8, dv + (uint64_t)(k * 128), idesc, (j > 0 || k > 0) ? 1u : 0u);   // 16 keys = 2 KB
+      mma_commit_elect(bar(KB_PV_DONE + 2 * t + sb));
+      mma_commit_elect(bar(KB_V_EMPTY + slot));
+    }
+    if (!ok) *abort_flag = 1;
+  } else {
+    // ------------------------------------------------------------------ softmax
+    {
+      uint4 u[HD / 8];
+      float top = 0.f;
+      const bf16* const qp = a.q + (size_t)(row0 + rr / G) * a.q_stride + (size_t)(kvh * G + rr % G) * HD;
+#pragma unroll
+      for (int x = 0; x < HD / 8; ++x) u[x] = row_live ? __ldcg(reinterpret_cast<const uint4*>(qp) + x) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int x = 0; x < HD / 8; ++x) {
+        float f[8];
+        unpack8(u[x], f);
+#pragma unroll
+        for (int y = 0; y < 8; ++y) top = fmaxf(top, fabsf(f[y]));
+      }
+      float up;
+      row_f = row_factor<HD>(top, up);
+#pragma unroll
+      for (int x = 0; x < HD / 8; ++x) {
+        float f[8];
+        unpack8(u[x], f);
+        const uint4 h = make_uint4(pack_f16(f[0] * up, f[1] * up), pack_f16(f[2] * up, f[3] * up), pack_f16(f[4] * up, f[5] * up), pack_f16(f[6] * up, f[7] * up));
+        *reinterpret_cast<uint4*>(base_ptr + g * Geo::Q_BYTES + (x >> 3) * KF_Q_HALF + row * 128 + (((x & 7) ^ (row & 7)) << 4)) = h;
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(KB_Q));
+    }
+    const uint32_t lane_base = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t s_addr = lane_base + KF_S_COL + g * 128, o_addr = lane_base + KF_O_COL + g * HD;
+    const int warp_rows = min(rows - g * KF_TILE - (warp & 3) * 32, 32);       // live ones
+    const int warp_r0 = r_first + g * KF_TILE + (warp & 3) * 32;
+    const int seen_least = seen0 + warp_r0 / G, seen_most = warp_rows > 0 ? seen0 + (warp_r0 + warp_rows - 1) / G : 0;
+    auto k_scale = [&](int i) { const int id = page_id(i); return id >= 0 ? a.scales[(size_t)id * 2 * a.Hkv + kvh] : 0.f; };
+    float ks_cur = k_scale(lane), ks_next = k_scale(32 + lane);        // of 8 steps each
+    for (int j = 0; j < steps && g < n_mt; ++j) {
+      const int sb = j & 1, k0 = t_begin + j * KF_STEP;
+      if ((j & 7) == 0 && j > 0) { ks_cur = ks_next; ks_next = k_scale((j + 8) * 4 + lane); }
+      if (!mbar_wait<false>(bar(KB_S_FULL + 2 * g + sb), (j >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 29); break; }
+      tc_fence_after();
+      const uint32_t addr = s_addr + sb * 64;
+      if (k0 >= seen_most) {                          // no row of the warp sees any of these keys
+        const uint32_t z[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int c = 0; c < 32; c += 8) kf_st8(addr + c, z);
+        kf_st_wait();
+      } else {
+        uint32_t v[64];
+        tmem_ld32_nowait(addr, v);
+        tmem_ld32_nowait(addr + 32, v + 32);
+        float f[4];
+#pragma unroll
+        for (int p = 0; p < 4; ++p) f[p] = fmaxf(row_f * __shfl_sync(0xffffffffu, ks_cur, (j & 7) * 4 + p), KV8_TINY_SCALE);
+        tmem_ld_wait();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_regs_ready16(v + 16 * c);
+        if (k0 + KF_STEP > seen_least) {              // some row's limit lies in this step
+#pragma unroll
+          for (int i = 0; i < 64; ++i) if (k0 + i >= seen) v[i] = 0xff800000u;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+          for (int i = 16 * p; i < 16 * p + 16; i += 4) {
+            m0 = kf_max3(m0, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
+            m1 = kf_max3(m1, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
+          }
+          mx = fmaxf(mx, fmaxf(m0, m1) * f[p]);
+        }
+        if (j == 0) {
+          m_ref = mx == -INFINITY ? 0.f : mx;         // (a row that sees a key of the chunk sees its first one)
+        } else if (__any_sync(0xffffffffu, row_live && mx - m_ref > KF_RAISE)) {
+          const float m_new = fmaxf(m_ref, mx), r = ex2(m_ref - m_new);
+          m_ref = m_new;
+          l *= r;
+          // every P V up to the step before must be complete
+          if (!mbar_wait<false>(bar(KB_PV_DONE + 2 * g + (sb ^ 1)), ((j - 1) >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 30); break; }
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < HD; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(o_addr + c, o);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * r);
+            kf_st8(o_addr + c, o);
+            kf_st8(o_addr + c + 8, o + 8);
+          }
+        }
+        const uint64_t nm = f2(-m_ref, -m_ref);
+        uint64_t la = 0, lb = 0;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const uint64_t ff = f2(f[p], f[p]);
+          uint32_t h[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float x, y;
+            un_f2(fma2(f2(__uint_as_float(v[16 * p + 2 * i]), __uint_as_float(v[16 * p + 2 * i + 1])), ff, nm), x, y);
+            x = ex2(x);
+            y = ex2(y);
+            if (i & 1) lb = add2(lb, f2(x, y)); else la = add2(la, f2(x, y));
+            h[i] = pack_f16(x, y);
+          }
+          kf_st8(addr + 8 * p, h);
+        }
+        float a0, a1, a2, a3;
+        un_f2(la, a0, a1);
+        un_f2(lb, a2, a3);
+        l += (a0 + a1) + (a2 + a3);
+        kf_st_wait();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(KB_P_READY + 2 * g + sb));
+    }
+    if (ok && g < n_mt && !mbar_wait<false>(bar(KB_PV_DONE + 2 * g + ((steps - 1) & 1)), ((steps - 1) >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 18); }
+    if (!ok) *abort_flag = 1;
+  }
+  __syncthreads();                                    // (what the converters found is there)
+  if (warp < 8 && g < n_mt && ok) {
+    // ------------------------------------------------------------------ output: a thread's row
+    tc_fence_after();
+    const uint32_t o_addr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + KF_O_COL + g * HD;
+    const bool nans = *any_nan != 0, direct = seen <= a.chunk;
+    const size_t qr = (size_t)(row0 + rr / G) * a.Hkv * G + kvh * G + rr % G;
+    bf16* const out = a.out + qr * HD;
+    float* const part = a.partial + (qr * a.max_chunks + chunk) * (HD + 2);
+    const float inv = direct ? v_ref / l : v_ref;
+    const bool write = row_live && seen > t_begin;
+#pragma unroll 1
+    for (int c = 0; c < HD; c += 32) {
+      uint32_t o[32];
+      tmem_ld32(o_addr + c, o);
+      if (write) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
+        if (nans) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) if (nan_key[c + i] < seen) o[i] = 0x7fffffffu;
+        }
+        if (!direct) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 2) __stcg(reinterpret_cast<float2*>(part + 2 + c + i), make_float2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])));
+        } else if ((reinterpret_cast<uintptr_t>(out) & 15) == 0) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            uint4 w;
+            w.x = pack2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])); w.y = pack2(__uint_as_float(o[i + 2]), __uint_as_float(o[i + 3]));
+            w.z = pack2(__uint_as_float(o[i + 4]), __uint_as_float(o[i + 5])); w.w = pack2(__uint_as_float(o[i + 6]), __uint_as_float(o[i + 7]));
+            *reinterpret_cast<uint4*>(out + c + i) = w;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) out[c + i] = f2bf(__uint_as_float(o[i]));
+        }
+      }
+      __syncwarp();
+    }
+    if (write && !direct) __stcg(reinterpret_cast<float2*>(part), make_float2(m_ref, l));
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == KF_S_WARP) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+  }
+}
+
+template <int HD>
+cudaError_t launch_as(const Kv8Attn& a, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(kv8_flash_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KfGeo<HD>::SMEM);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kv8_flash_kernel<HD>, dim3((unsigned)(a.B * a.Hkv * a.tiles), (unsigned)a.max_chunks), dim3(KF_THREADS), KfGeo<HD>::SMEM, st, a);
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_flash(const Kv8Attn& a, int hd, cudaStream_t st) { return hd == 128 ? launch_as<128>(a, st) : launch_as<64>(a, st); }
+
+}  // namespace epara
