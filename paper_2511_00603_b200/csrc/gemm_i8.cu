@@ -411,14 +411,14 @@ __device__ __forceinline__ void i8_epilogue(const I8Args& g, int m_base, int n0,
     if (n + CW <= g.N) {
 #pragma unroll
       for (int j = 0; j < CW; j += 4) {
-        const float4 w = __ldg(reinterpret_cast<const float4*>(g.w_scale + n + j));
+        const float4 w = *reinterpret_cast<const float4*>(g.w_scale + n + j);
         v[j] = scaled((int)r[j], as, w.x); v[j + 1] = scaled((int)r[j + 1], as, w.y);
         v[j + 2] = scaled((int)r[j + 2], as, w.z); v[j + 3] = scaled((int)r[j + 3], as, w.w);
       }
       if (g.epi & EPI_BIAS) {
 #pragma unroll
         for (int j = 0; j < CW; j += 8) {
-          const uint4 b = __ldg(reinterpret_cast<const uint4*>(g.bias + n + j));
+          const uint4 b = *reinterpret_cast<const uint4*>(g.bias + n + j);
           add_bias2(v[j], v[j + 1], b.x); add_bias2(v[j + 2], v[j + 3], b.y);
           add_bias2(v[j + 4], v[j + 5], b.z); add_bias2(v[j + 6], v[j + 7], b.w);
         }

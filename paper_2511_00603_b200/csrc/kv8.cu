@@ -126,17 +126,6 @@ __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8
 // out of the matrices: a page's K scale multiplies its scores, its V scale the probabilities, relative to the largest V scale
 // so far so that fp16 holds them.  Which dim a k index of the first product stands for, and which one a row of the second, is
 // free, and is chosen so that a lane reads 16 consecutive bytes of K and of V.
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 lds16(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
-}
 __device__ __forceinline__ uint2 lds8(uint32_t a) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");

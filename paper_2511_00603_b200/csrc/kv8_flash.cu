@@ -33,14 +33,17 @@ constexpr int KF_S_WARP = 8, KF_PV_WARP = 9, KF_CONV_WARP = 11, KF_CONV_WARPS = 
 constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
 constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
 constexpr float KF_RAISE = 8.0f;
+constexpr int KF_SORTED = 512;                        // requests of a call that are put in order
 
 template <int HD>
 struct KfGeo {
   static constexpr int NH = HD / 64;
   static constexpr int Q_BYTES = KF_Q_HALF * NH, KV_BYTES = KF_KV_HALF * NH;   // a tile of Q; a step's K or V
-  static constexpr int STAGES = HD == 64 ? 6 : 4;
+  static constexpr int STAGES = HD == 64 ? 4 : 3;                              // of converted K and V
+  static constexpr int RAW = 4, RAW_BYTES = 2 * EPARA_KV_PAGE * HD;            // pages that a converter has requested, K and V of one
   static constexpr int OFF_KV = 2 * Q_BYTES;
-  static constexpr int OFF_NAN = OFF_KV + STAGES * 2 * KV_BYTES;               // first key with a NaN in V, per dim
+  static constexpr int OFF_RAW = OFF_KV + STAGES * 2 * KV_BYTES;
+  static constexpr int OFF_NAN = OFF_RAW + KF_CONV_WARPS * RAW * RAW_BYTES;    // first key with a NaN in V, per dim
   static constexpr int OFF_BAR = OFF_NAN + HD * 4;
   static constexpr int SMEM = 1024 + OFF_BAR + 512;
   static_assert(SMEM <= 227 * 1024 && 2 * SMEM > 227 * 1024, "one CTA, which takes all of the tensor memory, to an SM");
@@ -111,9 +114,25 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   float* const v_tops = reinterpret_cast<float*>(tmem_slot + 3);      // [KF_CONV_WARPS]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  // ---- the work item; the longest ones, a request's last rows, come first
-  const int bk = blockIdx.x % (a.B * a.Hkv), pair = a.tiles - 1 - blockIdx.x / (a.B * a.Hkv), b = bk / a.Hkv, kvh = bk % a.Hkv, chunk = blockIdx.y;
+  // ---- the work item.  The longest ones start first: requests in order of their lengths, of each one the last rows first.  (In order of
+  // the rows alone a long request with few rows came late: XXX us for the four prompt chunks, like this XXX.)
+  const int kvh = blockIdx.x % a.Hkv, nth = blockIdx.x / a.Hkv / a.tiles, pair = a.tiles - 1 - blockIdx.x / a.Hkv % a.tiles, chunk = blockIdx.y;
+  __shared__ int the_request;
   pdl_wait();
+  int b = nth;
+  if (a.B > 1 && a.B <= KF_SORTED) {
+    for (int i = threadIdx.x; i < a.B; i += KF_THREADS) {
+      const int mine = a.kv_lens[i];
+      int before = 0;
+      for (int k = 0; k < a.B; ++k) {
+        const int other = a.kv_lens[k];
+        before += other > mine || (other == mine && k < i);
+      }
+      if (before == nth) the_request = i;
+    }
+    __syncthreads();
+    b = the_request;
+  }
   int row0, n;
   new_rows(a.q_rows, b, a.T, row0, n);
   const int G = a.G, len = min(max(a.kv_lens[b], 0), a.max_len);
@@ -179,26 +198,35 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   if (warp >= KF_CONV_WARP) {
     // ------------------------------------------------------------------ converters
     const int cw = warp - KF_CONV_WARP;               // this warp's page of a step
-    uint4 kx[NX], vx[NX];
     int id_cur = page_id(lane * 4 + cw), id_next = page_id((lane + 32) * 4 + cw);      // of 32 steps each
     auto scale_of = [&](int id) { return id >= 0 ? a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh] : 0.f; };
     float vs_cur = scale_of(id_cur), vs_next = scale_of(id_next);
-    int where[NX], place[NX];                         // of a piece in the page tile and in the converted tile (its first half)
+    // The pages of the next steps are requested as 16-byte asynchronous copies into a ring of this warp's own: a step is shorter than
+    // the way to memory (with one step's loads in registers 359 us for the four prompt chunks, like this XXX).
+    const uint32_t raw = base + Geo::OFF_RAW + cw * Geo::RAW * Geo::RAW_BYTES;
+    int where[NX], rawat[NX], place[NX];              // of a piece in the page tile, in the ring and in the converted tile (its first half)
 #pragma unroll
     for (int x = 0; x < NX; ++x) {
       const int half = HD == 128 ? x & 1 : 0, r = (HD == 128 ? x >> 1 : x) * 8 + (lane >> 2), R = cw * 16 + r;
       where[x] = r * HD + half * 64 + (lane & 3) * 16;
+      rawat[x] = HD == 128 ? where[x] ^ ((r & 1) << 6) : where[x];             // (rows in turn in different banks)
       place[x] = half * KF_KV_HALF + R * 128 + ((((lane & 3) * 2) ^ (R & 7)) << 4);
     }
-    auto load = [&](int j, int is_v, uint4* u) {
-      const int id = __shfl_sync(0xffffffffu, (j & 32) == 0 ? id_cur : id_next, j & 31);
+    auto request = [&](int j) {
+      if (j < steps) {
+        const int id = __shfl_sync(0xffffffffu, (j & 32) == 0 ? id_cur : id_next, j & 31);
+        const uint32_t dst = raw + (j % Geo::RAW) * Geo::RAW_BYTES;
+        const unsigned char* p = a.codes + ((size_t)max(id, 0) * 2 * a.Hkv + kvh) * EPARA_KV_PAGE * HD;
 #pragma unroll
-      for (int x = 0; x < NX; ++x) u[x] = make_uint4(0u, 0u, 0u, 0u);
-      if (j < steps && id >= 0) {
-        const unsigned char* p = a.codes + (((size_t)id * 2 + is_v) * a.Hkv + kvh) * EPARA_KV_PAGE * HD;
+        for (int kv = 0; kv < 2; ++kv)
 #pragma unroll
-        for (int x = 0; x < NX; ++x) u[x] = __ldg(reinterpret_cast<const uint4*>(p + where[x]));
+          for (int x = 0; x < NX; ++x) cp16_zfill(dst + kv * (EPARA_KV_PAGE * HD) + rawat[x], p + (size_t)kv * a.Hkv * EPARA_KV_PAGE * HD + where[x], id >= 0);
       }
+      cp_commit();
+    };
+    auto fetch = [&](int j, int is_v, uint4* u) {
+#pragma unroll
+      for (int x = 0; x < NX; ++x) u[x] = lds16(raw + (j % Geo::RAW) * Geo::RAW_BYTES + is_v * (EPARA_KV_PAGE * HD) + rawat[x]);
     };
     auto put = [&](unsigned char* tile, int x, const uint4& u, bool scaled, uint32_t f) {
       uint4 lo = make_uint4(to_f16x2(u.x), to_f16x2(u.x >> 16), to_f16x2(u.y), to_f16x2(u.y >> 16));
@@ -210,8 +238,8 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       *reinterpret_cast<uint4*>(tile + place[x]) = lo;
       *reinterpret_cast<uint4*>(tile + (place[x] ^ 16)) = hi;
     };
-    load(0, 0, kx);
-    load(0, 1, vx);
+#pragma unroll
+    for (int j = 0; j < Geo::RAW - 1; ++j) request(j);
     for (int j = 0; j < steps; ++j) {
       const int slot = j % ST;
       const uint32_t parity = ((j / ST) & 1u) ^ 1u;
@@ -220,13 +248,18 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
         if (j & 32) { id_cur = id; vs_cur = scale_of(id); } else { id_next = id; vs_next = scale_of(id); }
       }
       unsigned char* const kt = base_ptr + Geo::OFF_KV + slot * 2 * Geo::KV_BYTES;
+      request(j + Geo::RAW - 1);                      // into the place that the step before has left
+      cp_wait<Geo::RAW - 1>();
+      __syncwarp();
+      uint4 kx[NX], vx[NX];
+      fetch(j, 0, kx);
+      fetch(j, 1, vx);
       if (j >= ST && !mbar_wait(bar(KB_K_EMPTY + slot), parity, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 23); break; }
 #pragma unroll
       for (int x = 0; x < NX; ++x) put(kt, x, kx[x], false, 0u);
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(KB_K_FULL + slot));
-      load(j + 1, 0, kx);
       const float vs = __shfl_sync(0xffffffffu, (j & 32) == 0 ? vs_cur : vs_next, j & 31);
       const uint32_t vf = pack_f16(vs / v_ref, vs / v_ref);
       const int t0 = t_begin + j * KF_STEP + cw * 16;
@@ -258,7 +291,6 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(KB_V_FULL + slot));
-      load(j + 1, 1, vx);
     }
     if (!ok) *abort_flag = 1;
   } else if (warp == KF_S_WARP) {

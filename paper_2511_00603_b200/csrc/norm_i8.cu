@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(NV == most_groups(V) ? MOST_THREADS : 1024) rm
       const int c = (t + i * tpr) * V;
       if (a.gain != nullptr && c < a.d) {
         float g[V];
-        if constexpr (V == 8) unpack8(__ldg(reinterpret_cast<const uint4*>(a.gain + c)), g);
+        if constexpr (V == 8) unpack8(*reinterpret_cast<const uint4*>(a.gain + c), g);
         else g[0] = bf2f(a.gain[c]);
 #pragma unroll
         for (int e = 0; e < V; ++e) { ss = fmaf(h[i][e], h[i][e], ss); h[i][e] *= g[e]; }
