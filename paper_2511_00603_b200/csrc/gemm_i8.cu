@@ -1,12 +1,13 @@
 // int8 matrix product with a scale per token and per channel, C = epi((A W^T) a_scale[m] w_scale[n] + bias): int8 operands, exact
 // int32 sums (the order of K never shows), the scales applied in fp32 in the epilogue.
 //
-// Three kernels, as for the bf16 products and for the same reasons: rows of 128 bytes are 128 values here instead of 64, so a
+// Two kernels, as for the bf16 products and for the same reasons: rows of 128 bytes are 128 values here instead of 64, so a
 // k-block moves the same bytes and the tensor core does twice the work on them.
-//   stream  up to I8_STREAM_ROWS rows: one block per 16 rows of W over the whole K, mma.sync, bound by reading W once;
-//   swap    a tile of 128 rows of W is the MMA's M and up to 256 batch rows its N, K in ranges over a cluster whose
-//           partial sums meet in distributed shared memory;
+//   swap    few rows, bound by reading W once or by latency: a tile of 128 rows of W is the MMA's M and 16 to 256 batch rows its N, K
+//           in ranges over a cluster whose partial sums meet in distributed shared memory;
 //   pair    256-row tiles on pairs of CTAs, persistent, two accumulators.
+// (A third one for up to 16 rows on mma.sync, as for bf16, was slower here: 1 x 32000 x 4096 35 us, swapped operands 23;
+// 16 x 6144 x 4096 11.4 and 8.8; 1 x 6144 x 4096 9.0 and 8.5.)
 // Operands come by plain TMA (columns past K and rows past the matrix arrive as zeros), products run as tcgen05.mma kind::i8,
 // sums are in tensor memory.  Every wait is bounded; a kernel that gives up leaves a code in *status.
 #include <algorithm>
@@ -24,14 +25,12 @@ using namespace tc;
 
 struct alignas(64) I8Args {
   CUtensorMap tmA, tmW;
-  const int8_t* A;
-  const int8_t* W;
   const float* a_scale;
   const float* w_scale;
   const bf16* bias;
   void* C;
   int* status;
-  int M, N, K, lda, ldw, ldc, epi;
+  int M, N, K, ldc, epi;
   int bn;                // swap: batch rows of a tile; pair: columns
   int tiles_m, tiles_n;
   int vec;               // rows of C start on 16 bytes (swap: on four elements)
@@ -58,100 +57,6 @@ __device__ __forceinline__ void mma_i8_pair_elect(uint32_t tmem_d, uint64_t da, 
 
 // The roundings are spelled out: an output has the same bits whichever kernel its batch runs on.
 __device__ __forceinline__ float scaled(int sum, float a, float w) { return __fmul_rn(__fmul_rn((float)sum, a), w); }
-
-// ------------------------------------------------------------------------------------------------ stream
-constexpr int ST_ROWS = 16, ST_WARPS = 16, ST_U = 4;
-
-__device__ __forceinline__ uint4 ldg_w(const int8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ void mma_s8(int* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// the first `n` bytes of 16, the others zero
-__device__ __forceinline__ uint4 first_bytes(uint4 v, int n) {
-  auto m = [&](int w) { const int k = n - 4 * w; return k >= 4 ? 0xffffffffu : k <= 0 ? 0u : (1u << (8 * k)) - 1u; };
-  v.x &= m(0); v.y &= m(1); v.z &= m(2); v.w &= m(3);
-  return v;
-}
-
-// K is cut into k-blocks of 64 values dealt to the warps in turn; in one, lane (gq, tq) holds 16 consecutive values of W rows gq and
-// gq + 8 and of activation row gq, the operands of two m16n8k32 with W as the 16 rows and the batch as the 8 columns.  (The k
-// order inside an MMA is a permutation of memory order, the same for both.)
-template <int NT>
-__global__ void __launch_bounds__(ST_WARPS * 32) gemm_i8_stream_kernel(const __grid_constant__ I8Args g) {
-  __shared__ int red[ST_WARPS][NT][ST_ROWS][9];
-  __shared__ float outv[NT][8][ST_ROWS];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
-  const int n0 = blockIdx.x * ST_ROWS, N = g.N, M = g.M, K = g.K;
-  pdl_wait();
-  const int kblocks = (K + 63) / 64;
-  const int8_t* const w_lo = g.W + (size_t)min(n0 + gq, N - 1) * g.ldw + tq * 16;
-  const int8_t* const w_hi = g.W + (size_t)min(n0 + gq + 8, N - 1) * g.ldw + tq * 16;
-  int acc[NT][4];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0;
-  for (int kb0 = warp; kb0 < kblocks; kb0 += ST_WARPS * ST_U) {
-    uint4 wl[ST_U], wh[ST_U], xv[NT][ST_U];
-#pragma unroll
-    for (int u = 0; u < ST_U; ++u) {
-      const int k = (kb0 + u * ST_WARPS) * 64;
-      wl[u] = wh[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (k + tq * 16 < K) { wl[u] = ldg_w(w_lo + k); wh[u] = ldg_w(w_hi + k); }
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int u = 0; u < ST_U; ++u) {
-        const int k = (kb0 + u * ST_WARPS) * 64, left = K - k - tq * 16, m = t * 8 + gq;
-        xv[t][u] = make_uint4(0u, 0u, 0u, 0u);
-        if (left > 0 && m < M) xv[t][u] = __ldcg(reinterpret_cast<const uint4*>(g.A + (size_t)m * g.lda + k + tq * 16));
-        if (left < 16) xv[t][u] = first_bytes(xv[t][u], left);     // the pad behind a row's K values may hold anything
-      }
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int u = 0; u < ST_U; ++u) {
-        mma_s8(acc[t], wl[u].x, wh[u].x, wl[u].y, wh[u].y, xv[t][u].x, xv[t][u].y);
-        mma_s8(acc[t], wl[u].z, wh[u].z, wl[u].w, wh[u].w, xv[t][u].z, xv[t][u].w);
-      }
-  }
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    red[warp][t][gq][2 * tq] = acc[t][0];
-    red[warp][t][gq][2 * tq + 1] = acc[t][1];
-    red[warp][t][gq + 8][2 * tq] = acc[t][2];
-    red[warp][t][gq + 8][2 * tq + 1] = acc[t][3];
-  }
-  __syncthreads();
-  const int epi = g.epi;
-  for (int idx = threadIdx.x; idx < NT * 8 * ST_ROWS; idx += ST_WARPS * 32) {
-    const int r = idx % ST_ROWS, bm = (idx / ST_ROWS) % 8, t = idx / (ST_ROWS * 8), n = n0 + r, m = t * 8 + bm;
-    int s = 0;
-#pragma unroll
-    for (int w = 0; w < ST_WARPS; ++w) s += red[w][t][r][bm];
-    float v = 0.f;
-    if (n < N && m < M) {
-      v = scaled(s, g.a_scale[m], g.w_scale[n]);
-      if (epi & EPI_BIAS) v = __fadd_rn(v, bf2f(g.bias[n]));
-      if (epi & EPI_GELU) v = gelu_erf(v);
-    }
-    outv[t][bm][r] = v;
-  }
-  __syncthreads();
-  for (int idx = threadIdx.x; idx < NT * 8 * ST_ROWS; idx += ST_WARPS * 32) {
-    const int r = idx % ST_ROWS, bm = (idx / ST_ROWS) % 8, t = idx / (ST_ROWS * 8), m = t * 8 + bm, n = n0 + r;
-    if (m >= M || n >= N) continue;
-    const float v = outv[t][bm][r];
-    if (epi & EPI_RESID_F32) static_cast<float*>(g.C)[(size_t)m * g.ldc + n] += v;     // (v comes from shared memory: no fused addition)
-    else if (epi & EPI_SWIGLU) {
-      if ((r & 1) == 0) static_cast<bf16*>(g.C)[(size_t)m * g.ldc + (n >> 1)] = f2bf(silu_f(v) * outv[t][bm][r + 1]);
-    } else static_cast<bf16*>(g.C)[(size_t)m * g.ldc + n] = f2bf(v);
-  }
-}
 
 // ------------------------------------------------------------------------------------------------ swap
 constexpr int SW_BM = 128, SW_W_BYTES = SW_BM * KB;                // 16 KB
@@ -615,34 +520,49 @@ bool make_i8_map(CUtensorMap* tm, const void* p, long long rows, long long cols,
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-constexpr int I8_STREAM_ROWS = 16;
-
-enum { I8_STREAM, I8_SWAP, I8_PAIR };
+enum { I8_SWAP, I8_PAIR };
 struct I8Plan { int kernel, bn, split; };
 
+inline int swap_ring(int bn, long long ctas, int split, int sm_count) { return bn <= 128 && (ctas > sm_count || split == 8) ? SW_RING_2 : SW_RING_1; }
+
+// The kernel and its tile by an estimate of the time in microseconds, whose terms are: a launch and its set-up; what an SM takes in, 105
+// KB a microsecond, against what HBM delivers of W, 6 MB a microsecond (4.6 where two CTAs with wide tiles share an SM: their rings
+// are short); and for swapped operands 0.8 for every 32 rows that a CTA writes out and 0.3 and 20 ns a row for the exchange.  Device
+// times of calls in a row with W cold, measured (estimate), swapped operands: 1 x 6144 x 4096 one range 9.5 (9.3), two 8.5 (8.6), four 8.6 (8.6);
+// 32 x 4096 x 14336 two ranges 15.4 (15.4), four 14.0 (14.5); 394 x 1000 x 776 tiles of 32 rows 5.3 (5.1), of 64 with two ranges 6.0 (6.3),
+// of 208 with two 11 (12.3); 128 x 4096 x 14336 with four 16.8 (16.4); 256 x 6144 x 4096 tiles of 96 rows 12.8 (13.9), pairs, 128 columns
+// 11.6 (11.6); 512 x 4096 x 4096 14.1 (16.0) and 12.3 (11.6); 96 x 28672 x 4096 31 (31), pairs, 256 columns 28 (27).
 I8Plan i8_plan(long long M, int N, int K, int sm_count) {
-  I8Plan p = {I8_STREAM, 0, 1};
-  if (M <= I8_STREAM_ROWS) return p;
   const int kblocks = (K + KB - 1) / KB;
-  if (M <= 512) {
-    const int tiles_m = (int)((M + SW_TILE_ROWS - 1) / SW_TILE_ROWS), tiles = (N + SW_BM - 1) / SW_BM * tiles_m;
-    p.kernel = I8_SWAP;
-    p.bn = (int)(((M + tiles_m - 1) / tiles_m + 15) / 16 * 16);
-    const int fit = p.bn <= 128 ? 2 * sm_count : sm_count;
-    while (p.split < 8 && tiles * p.split * 2 <= fit && kblocks / (p.split * 2) >= (p.split == 4 ? 8 : 2)) p.split *= 2;
-    return p;
+  const double w_mb = (double)N * K * 1e-6;
+  I8Plan p = {I8_PAIR, 256, 1};
+  double best = 1e30;
+  for (int bn = 128; bn <= 256; bn += 128) {
+    const long long tiles = (M + 255) / 256 * ((N + bn - 1) / bn), pairs = sm_count / 2, rounds = (tiles + pairs - 1) / pairs;
+    const double t = 4.6 + std::max((double)rounds * kblocks * (bn == 256 ? 0.34 : 0.22), w_mb / 6.0) + 0.3 * (double)(rounds - 1);
+    if (t < best) { best = t; p.bn = bn; }
   }
-  p.kernel = I8_PAIR;
-  const long long tiles_m = (M + 255) / 256, pairs = sm_count / 2;
-  auto rounds = [&](int bn) { return (tiles_m * ((N + bn - 1) / bn) + pairs - 1) / pairs; };
-  p.bn = rounds(128) * 0.8 < rounds(256) * 1.0 && rounds(256) <= 2 ? 128 : 256;
+  if (M > 1024) return p;
+  const int tiles_n = (N + SW_BM - 1) / SW_BM;
+  for (int tiles_m = (int)((M + SW_TILE_ROWS - 1) / SW_TILE_ROWS); tiles_m <= 32; ++tiles_m) {
+    const int bn = (int)(((M + tiles_m - 1) / tiles_m + 15) / 16 * 16);
+    if (tiles_m > 1 && bn < 32) break;
+    for (int s = 1; s <= 8 && s <= kblocks; s *= 2) {
+      const long long ctas = (long long)tiles_n * ((M + bn - 1) / bn) * s, per_sm = (ctas + sm_count - 1) / sm_count;
+      const bool two = swap_ring(bn, ctas, s, sm_count) == SW_RING_2;
+      const double main = (double)per_sm * ((kblocks + s - 1) / s) * (16.0 + bn / 8.0) / 105.0, hbm = w_mb / (two && bn > 64 ? 4.6 : 6.0);
+      const double out = 0.8 * ((bn + 32 * s - 1) / (32 * s)) + (s > 1 ? 0.3 + 0.02 * bn : 0.0) + (s == 8 ? 0.6 : 0.0);
+      const double t = 3.0 + std::max(main, hbm) + out * (double)(two ? (per_sm + 1) / 2 : per_sm);
+      if (t < best) { best = t; p.kernel = I8_SWAP; p.bn = bn; p.split = s; }
+    }
+  }
   return p;
 }
 
 template <int S>
 cudaError_t launch_i8_swap(const I8Args& g, int sm_count, cudaStream_t st) {
   const int tiles = g.tiles_m * g.tiles_n;
-  const int ring = g.bn <= 128 && (tiles * S > sm_count || S == 8) ? SW_RING_2 : SW_RING_1;
+  const int ring = swap_ring(g.bn, (long long)tiles * S, S, sm_count);
   cudaError_t e = cudaFuncSetAttribute(gemm_i8_swap_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sw_smem(SW_RING_1));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -685,14 +605,11 @@ extern "C" int epara_gemm_i8(int device, void* cuda_stream, const epara_gemm_i8_
   const int sm = device_sm_count(device);
   const I8Plan plan = i8_plan(q.M, q.N, q.K, sm);
   I8Args g;
-  g.A = (const int8_t*)q.A; g.W = (const int8_t*)q.W; g.a_scale = q.a_scale; g.w_scale = q.w_scale; g.bias = (const bf16*)q.bias; g.C = q.C; g.status = status;
-  g.M = q.M; g.N = q.N; g.K = q.K; g.lda = q.lda; g.ldw = q.ldw; g.ldc = q.ldc; g.epi = q.epilogue;
+  g.a_scale = q.a_scale; g.w_scale = q.w_scale; g.bias = (const bf16*)q.bias; g.C = q.C; g.status = status;
+  g.M = q.M; g.N = q.N; g.K = q.K; g.ldc = q.ldc; g.epi = q.epilogue;
   g.bn = plan.bn; g.tiles_m = g.tiles_n = 1; g.vec = 0;
   cudaError_t e;
-  if (plan.kernel == I8_STREAM) {
-    const dim3 grid((unsigned)((q.N + ST_ROWS - 1) / ST_ROWS)), block(ST_WARPS * 32);
-    e = q.M <= 8 ? launch_pdl(gemm_i8_stream_kernel<1>, grid, block, 0, st, g) : launch_pdl(gemm_i8_stream_kernel<2>, grid, block, 0, st, g);
-  } else if (plan.kernel == I8_SWAP) {
+  if (plan.kernel == I8_SWAP) {
     g.tiles_m = (q.M + g.bn - 1) / g.bn;
     g.tiles_n = (q.N + SW_BM - 1) / SW_BM;
     g.vec = q.ldc % (swi ? 2 : 4) == 0;
