@@ -157,16 +157,34 @@ __device__ __forceinline__ int v_piece(int r, int p) {
 }
 
 constexpr int KV8_WARPS = 4;
+constexpr int KV8_CLUSTER = 8;                     // most chunks that a cluster merges
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t mapa_cluster(uint32_t addr, int rank) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float2 ld_cluster(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+  return v;
+}
 template <int HD, int NT>
 struct Kv8Geo {
-  static constexpr int STAGES = HD == 128 && NT == 1 ? 3 : 4, BLOCKS = NT == 1 ? 4 : 3;     // pages in a warp's ring, blocks to an SM
-  static constexpr int RING = KV8_WARPS * STAGES * 2 * PAGE * HD, MERGE = KV8_WARPS * 8 * NT * HD * 4, SMEM = RING > MERGE ? RING : MERGE;
+  // pages that a warp takes at once (hd 64: what a step costs beside its products is paid for two), steps in its ring, blocks to an SM
+  static constexpr int PAGES = HD == 64 ? 2 : 1, STAGES = NT == 1 ? 3 : 4, BLOCKS = NT == 1 ? 4 : 3;
+  static constexpr int RING = KV8_WARPS * STAGES * PAGES * 2 * PAGE * HD, MERGE = KV8_WARPS * 8 * NT * HD * 4;
+  static constexpr int MERGED = MERGE + 8 * NT * (HD + 2) * 4, SMEM = RING > MERGED ? RING : MERGED;       // ... and the block's own result behind it
 };
 
-template <int HD, int NT>
+// CLUSTER: the chunks of a tile are the blocks of a cluster, which merge their results through distributed shared memory; without
+// it results of several chunks go to scratch and a second kernel merges them.
+template <int HD, int NT, bool CLUSTER>
 __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_attn_kernel(const Kv8Attn a) {
   constexpr int KK = HD / 64, MT = HD / 16;        // 64-wide pieces of a row; m tiles of O^T
-  constexpr int TILE = PAGE * HD, ST = Kv8Geo<HD, NT>::STAGES, TR = 8 * NT;
+  constexpr int TILE = PAGE * HD, ST = Kv8Geo<HD, NT>::STAGES, PP = Kv8Geo<HD, NT>::PAGES, TR = 8 * NT;
   extern __shared__ __align__(128) unsigned char ring[];
   __shared__ float sm_m[KV8_WARPS][TR], sm_l[KV8_WARPS][TR];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, tq = lane & 3;
@@ -184,7 +202,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   if (rows <= 0) return;
   const int seen_top = seen0 + (tile * TR + rows - 1) / G;
   const int t_begin = chunk * a.chunk, t_end = min(seen_top, t_begin + a.chunk);
-  if (t_begin >= t_end) return;
+  if (!CLUSTER && t_begin >= t_end) return;        // (a block of a cluster goes on with no pages)
   int seen[NT][2];                                 // tokens seen by this thread's rows 8 y + 2 tq + {0, 1}
 #pragma unroll
   for (int y = 0; y < NT; ++y)
@@ -195,15 +213,15 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
     }
   const int seen_least = min(seen0 + tile * TR / G, t_end);        // pages up to here are whole for every row
 
-  // ---- the pages of this warp: lanes hold the ids and scales of 32 of them, and of the 32 after those (by parity)
+  // ---- the steps of this warp, PP pages each: lanes hold the ids and scales of 32 pages, and of the 32 after those (by parity)
   const int32_t* const table = a.tables + (size_t)b * a.table_stride;
-  const int pg0 = t_begin / PAGE + warp, pg_end = (t_end + PAGE - 1) / PAGE;
-  const int n_pages = pg0 < pg_end ? (pg_end - pg0 + KV8_WARPS - 1) / KV8_WARPS : 0;
+  const int step0 = t_begin / (PAGE * PP) + warp, pg_end = (t_end + PAGE - 1) / PAGE, step_end = (pg_end + PP - 1) / PP;
+  const int n_steps = step0 < step_end ? (step_end - step0 + KV8_WARPS - 1) / KV8_WARPS : 0;
   auto load_id = [&](int batch) {
-    const int i = batch * 32 + lane;
+    const int i = batch * 32 + lane, pg = (step0 + i / PP * KV8_WARPS) * PP + i % PP;
     int id = -1;
-    if (i < n_pages) {
-      id = table[pg0 + i * KV8_WARPS];
+    if (pg < pg_end) {
+      id = table[pg];
       if (id < 0 || id >= a.kv_pages) { atomicExch(a.status, ERR_PAGE_ATTEND); id = -1; }
     }
     return id;
@@ -217,7 +235,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
     return s;
   };
   int id_even = load_id(0), id_odd = load_id(1);
-  const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(ring) + warp * ST * 2 * TILE;
+  const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(ring) + warp * ST * PP * 2 * TILE;
   uint32_t k_dst[TILE / 512], v_dst[TILE / 512];
 #pragma unroll
   for (int x = 0; x < TILE / 512; ++x) {
@@ -225,18 +243,21 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
     k_dst[x] = k_piece<HD>(r, p);
     v_dst[x] = TILE + v_piece<HD>(r, p);
   }
-  int fill = 0;                                    // stage of the next page to request
-  auto issue = [&](int i) {                        // page i of this warp into its stage (one commit group each, empty ones too)
-    if (i < n_pages) {
-      const int id = __shfl_sync(0xffffffffu, (i & 32) == 0 ? id_even : id_odd, i & 31);
-      if (id >= 0) {
-        const uint32_t dst = my_ring + fill * 2 * TILE;
-        const unsigned char* k = a.codes + ((size_t)id * 2 * a.Hkv + kvh) * TILE + lane * 16;
-        const unsigned char* v = k + (size_t)a.Hkv * TILE;
+  int fill = 0;                                    // stage of the next step to request
+  auto issue = [&](int i) {                        // a step's pages into their stage (one commit group each, empty ones too)
+    if (i < n_steps) {
 #pragma unroll
-        for (int x = 0; x < TILE / 512; ++x) cp16(dst + k_dst[x], k + x * 512);
+      for (int p = 0; p < PP; ++p) {
+        const int at = i * PP + p, id = __shfl_sync(0xffffffffu, (at & 32) == 0 ? id_even : id_odd, at & 31);
+        if (id >= 0) {
+          const uint32_t dst = my_ring + (fill * PP + p) * 2 * TILE;
+          const unsigned char* k = a.codes + ((size_t)id * 2 * a.Hkv + kvh) * TILE + lane * 16;
+          const unsigned char* v = k + (size_t)a.Hkv * TILE;
 #pragma unroll
-        for (int x = 0; x < TILE / 512; ++x) cp16(dst + v_dst[x], v + x * 512);
+          for (int x = 0; x < TILE / 512; ++x) cp16(dst + k_dst[x], k + x * 512);
+#pragma unroll
+          for (int x = 0; x < TILE / 512; ++x) cp16(dst + v_dst[x], v + x * 512);
+        }
       }
     }
     cp_commit();
@@ -297,13 +318,14 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   }
 
   int stage = 0;
-  for (int i = 0; i < n_pages; ++i) {
-    if ((i & 31) == 0) {
+  for (int i = 0; i < n_steps; ++i) {
+    const bool even = (i * PP & 32) == 0;
+    if ((i * PP & 31) == 0) {
       if (i > 0) {                                 // the 32 pages after the next ones
-        if (i & 32) { id_even = load_id(i / 32 + 1); sc_even = load_scales(id_even); }
-        else { id_odd = load_id(i / 32 + 1); sc_odd = load_scales(id_odd); }
+        if (even) { id_odd = load_id(i * PP / 32 + 1); sc_odd = load_scales(id_odd); }
+        else { id_even = load_id(i * PP / 32 + 1); sc_even = load_scales(id_even); }
       }
-      float top = (i & 32) == 0 ? sc_even.y : sc_odd.y;
+      float top = even ? sc_even.y : sc_odd.y;
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
       if (top > v_ref) {
@@ -316,20 +338,29 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         inv_ref = 1.f / top;
       }
     }
-    const int id = __shfl_sync(0xffffffffu, (i & 32) == 0 ? id_even : id_odd, i & 31);
-    const float ks = __shfl_sync(0xffffffffu, (i & 32) == 0 ? sc_even.x : sc_odd.x, i & 31);
-    const float vf = __shfl_sync(0xffffffffu, (i & 32) == 0 ? sc_even.y : sc_odd.y, i & 31) * inv_ref;
-    issue(i + ST - 1);                             // into the stage that the page before this one has left
+    bool there[PP];                                // pages of the pool
+    float ks[PP], vf[PP];
+#pragma unroll
+    for (int p = 0; p < PP; ++p) {
+      const int at = (i * PP + p) & 31;
+      there[p] = __shfl_sync(0xffffffffu, even ? id_even : id_odd, at) >= 0;
+      ks[p] = __shfl_sync(0xffffffffu, even ? sc_even.x : sc_odd.x, at);
+      vf[p] = __shfl_sync(0xffffffffu, even ? sc_even.y : sc_odd.y, at) * inv_ref;
+    }
+    issue(i + ST - 1);                             // into the stage that the step before this one has left
     cp_wait<ST - 1>();
     __syncwarp();
-    const uint32_t kt = my_ring + stage * 2 * TILE, vt = kt + TILE;
+    const uint32_t tiles = my_ring + stage * PP * 2 * TILE;
     if (++stage == ST) stage = 0;
-    if (id >= 0) {
-      const int t0 = (pg0 + i * KV8_WARPS) * PAGE;
-      // S^T: rows gq and gq + 8 are tokens t0 + gq and t0 + gq + 8, columns 2 tq + {0, 1} query rows
-      float s[NT][4];
+    const int t0 = (step0 + i * KV8_WARPS) * PP * PAGE;
+    const bool whole = t0 + PP * PAGE <= seen_least && there[0] && there[PP - 1];
+    // S^T: rows gq and gq + 8 are tokens t0 + gq and t0 + gq + 8 (page p: 16 more), columns 2 tq + {0, 1} query rows
+    float s[PP][NT][4];
 #pragma unroll
-      for (int y = 0; y < NT; ++y) s[y][0] = s[y][1] = s[y][2] = s[y][3] = 0.f;
+    for (int p = 0; p < PP; ++p) {
+      const uint32_t kt = tiles + p * 2 * TILE;
+#pragma unroll
+      for (int y = 0; y < NT; ++y) s[p][y][0] = s[p][y][1] = s[p][y][2] = s[p][y][3] = 0.f;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
         const uint4 lo = lds16(kt + k_piece<HD>(gq, kk * 4 + tq)), hi = lds16(kt + k_piece<HD>(gq + 8, kk * 4 + tq));
@@ -337,51 +368,61 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         for (int j = 0; j < 4; ++j) {
           const uint32_t a0 = to_f16x2(u4(lo, j)), a1 = to_f16x2(u4(hi, j)), a2 = to_f16x2(u4(lo, j) >> 16), a3 = to_f16x2(u4(hi, j) >> 16);
 #pragma unroll
-          for (int y = 0; y < NT; ++y) mma_f16(s[y], a0, a1, a2, a3, q[y][kk * 4 + j][0], q[y][kk * 4 + j][1]);
+          for (int y = 0; y < NT; ++y) mma_f16(s[p][y], a0, a1, a2, a3, q[y][kk * 4 + j][0], q[y][kk * 4 + j][1]);
         }
       }
-      const bool whole = t0 + PAGE <= seen_least;
-      bool raise = false;
 #pragma unroll
       for (int y = 0; y < NT; ++y) {
-        const float f0 = row_f[y][0] * ks, f1 = row_f[y][1] * ks;
-        s[y][0] *= f0; s[y][1] *= f1; s[y][2] *= f0; s[y][3] *= f1;          // to the log2 domain
+        const float f0 = row_f[y][0] * ks[p], f1 = row_f[y][1] * ks[p];
+        s[p][y][0] *= f0; s[p][y][1] *= f1; s[p][y][2] *= f0; s[p][y][3] *= f1;          // to the log2 domain
       }
-      if (!whole) {
+      if (!whole) {                                // (a page that is not there is not attended to, whatever its stage holds)
 #pragma unroll
         for (int y = 0; y < NT; ++y)
 #pragma unroll
-          for (int c = 0; c < 4; ++c) if (t0 + gq + 8 * (c >> 1) >= seen[y][c & 1]) s[y][c] = -INFINITY;
+          for (int c = 0; c < 4; ++c) if (!there[p] || t0 + p * PAGE + gq + 8 * (c >> 1) >= seen[y][c & 1]) s[p][y][c] = -INFINITY;
       }
-      // the running maximum is only raised when a score passes it by more than 2^8
+    }
+    // the running maximum is only raised when a score passes it by more than 2^8
+    float top[NT][2];
+    bool raise = false;
 #pragma unroll
-      for (int y = 0; y < NT; ++y) raise |= fmaxf(s[y][0], s[y][2]) > m[y][0] + 8.f || fmaxf(s[y][1], s[y][3]) > m[y][1] + 8.f;
-      if (__any_sync(0xffffffffu, raise)) {
+    for (int y = 0; y < NT; ++y)
 #pragma unroll
-        for (int y = 0; y < NT; ++y)
+      for (int e = 0; e < 2; ++e) {
+        top[y][e] = fmaxf(s[0][y][e], s[0][y][2 + e]);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float top = fmaxf(s[y][e], s[y][2 + e]);
+        for (int p = 1; p < PP; ++p) top[y][e] = fmaxf(top[y][e], fmaxf(s[p][y][e], s[p][y][2 + e]));
+        raise |= top[y][e] > m[y][e] + 8.f;
+      }
+    if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-            if (top > m[y][e]) {
-              const float f = ex2(m[y][e] - top);
-              m[y][e] = top;
-              l[y][e] *= f;
+      for (int y = 0; y < NT; ++y)
 #pragma unroll
-              for (int j = 0; j < MT; ++j) { o[y][j][e] *= f; o[y][j][2 + e] *= f; }
-            }
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) top[y][e] = fmaxf(top[y][e], __shfl_xor_sync(0xffffffffu, top[y][e], x));
+          if (top[y][e] > m[y][e]) {
+            const float f = ex2(m[y][e] - top[y][e]);
+            m[y][e] = top[y][e];
+            l[y][e] *= f;
+#pragma unroll
+            for (int j = 0; j < MT; ++j) { o[y][j][e] *= f; o[y][j][2 + e] *= f; }
           }
-      }
-      uint32_t p[NT][2];                           // P^T as the B operand
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < PP; ++p) {
+      const uint32_t vt = tiles + p * 2 * TILE + TILE;
+      uint32_t pt[NT][2];                          // P^T as the B operand
 #pragma unroll
       for (int y = 0; y < NT; ++y) {
         const float m0 = m[y][0] == -INFINITY ? 0.f : m[y][0], m1 = m[y][1] == -INFINITY ? 0.f : m[y][1];
-        const float p0 = ex2(s[y][0] - m0), p1 = ex2(s[y][1] - m1), p2 = ex2(s[y][2] - m0), p3 = ex2(s[y][3] - m1);
+        const float p0 = ex2(s[p][y][0] - m0), p1 = ex2(s[p][y][1] - m1), p2 = ex2(s[p][y][2] - m0), p3 = ex2(s[p][y][3] - m1);
         l[y][0] += p0 + p2;
         l[y][1] += p1 + p3;
-        p[y][0] = transpose_8x8(pack_f16(p0 * vf, p1 * vf));
-        p[y][1] = transpose_8x8(pack_f16(p2 * vf, p3 * vf));
+        pt[y][0] = transpose_8x8(pack_f16(p0 * vf[p], p1 * vf[p]));
+        pt[y][1] = transpose_8x8(pack_f16(p2 * vf[p], p3 * vf[p]));
       }
       // V^T as the A operand: bytes of two tokens interleaved, then two codes at a time to fp16; k indices 2 tq + {0, 1} and + 8 are
       // those tokens, rows gq and gq + 8 of m tile j the dims gq HD / 8 + 2 j + {0, 1}
@@ -401,7 +442,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         bool odd = false;                          // NaN codes that not every row sees
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          if (t0 + 2 * tq + (x & 1) + 8 * (x >> 1) >= t_end) {     // slots behind the last token may hold anything
+          if (!there[p] || t0 + p * PAGE + 2 * tq + (x & 1) + 8 * (x >> 1) >= t_end) {     // slots behind the last token may hold anything
 #pragma unroll
             for (int z = 0; z < HD / 32; ++z) w[x][z] = 0u;
           }
@@ -416,7 +457,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
           for (int y = 0; y < NT; ++y)
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              const int t = t0 + gq + 8 * x;
+              const int t = t0 + p * PAGE + gq + 8 * x;
               see[y][x] = transpose_8x8((t < seen[y][0] ? 0x3c00u : 0u) | (t < seen[y][1] ? 0x3c000000u : 0u));
             }
 #pragma unroll
@@ -449,7 +490,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
           const uint32_t b0 = __byte_perm(w[0][z], w[1][z], h ? 0x7362 : 0x5140), b1 = __byte_perm(w[2][z], w[3][z], h ? 0x7362 : 0x5140);
           const uint32_t a0 = to_f16x2(b0), a1 = to_f16x2(b0 >> 16), a2 = to_f16x2(b1), a3 = to_f16x2(b1 >> 16);
 #pragma unroll
-          for (int y = 0; y < NT; ++y) mma_f16(o[y][2 * z + h], a0, a1, a2, a3, p[y][0], p[y][1]);
+          for (int y = 0; y < NT; ++y) mma_f16(o[y][2 * z + h], a0, a1, a2, a3, pt[y][0], pt[y][1]);
         }
     }
     __syncwarp();                                  // the stage may be filled again
@@ -476,10 +517,21 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         *reinterpret_cast<float2*>(sm_o + (warp * TR + r) * HD + gq * (HD / 8) + 2 * j) = make_float2(o[y][j][e] * v_ref, o[y][j][2 + e] * v_ref);
     }
   __syncthreads();
+  float* const own = sm_o + KV8_WARPS * TR * HD;                   // CLUSTER: [row][maximum, sum, dims]
+  auto store = [&](size_t qr, int d, float x, float y) {
+    bf16* const out = a.out + qr * HD + d;
+    if ((reinterpret_cast<uintptr_t>(out) & 3) == 0) {
+      *reinterpret_cast<uint32_t*>(out) = pack2(x, y);
+    } else {
+      out[0] = f2bf(x);
+      out[1] = f2bf(y);
+    }
+  };
+  auto q_row = [&](int r) { return (size_t)(row0 + (tile * TR + r) / G) * a.Hkv * G + kvh * G + (tile * TR + r) % G; };
   for (int idx = threadIdx.x; idx < rows * (HD / 2); idx += KV8_WARPS * 32) {
-    const int r = idx / (HD / 2), d = idx % (HD / 2) * 2, rr = tile * TR + r;
-    const int sees = seen0 + rr / G;
-    if (sees <= t_begin) continue;
+    const int r = idx / (HD / 2), d = idx % (HD / 2) * 2;
+    const int sees = seen0 + (tile * TR + r) / G;
+    if (!CLUSTER && sees <= t_begin) continue;
     float mm = sm_m[0][r];
 #pragma unroll
     for (int w = 1; w < KV8_WARPS; ++w) mm = fmaxf(mm, sm_m[w][r]);
@@ -493,20 +545,47 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
       ox += ow.x * f;
       oy += ow.y * f;
     }
-    const size_t qr = (size_t)(row0 + rr / G) * a.Hkv * G + kvh * G + rr % G;
-    if (sees <= a.chunk) {
-      bf16* const out = a.out + qr * HD + d;
-      if ((reinterpret_cast<uintptr_t>(out) & 3) == 0) {
-        *reinterpret_cast<uint32_t*>(out) = pack2(ox / ll, oy / ll);
-      } else {
-        out[0] = f2bf(ox / ll);
-        out[1] = f2bf(oy / ll);
-      }
+    if (CLUSTER) {
+      *reinterpret_cast<float2*>(own + r * (HD + 2) + 2 + d) = make_float2(ox, oy);
+      if (d == 0) *reinterpret_cast<float2*>(own + r * (HD + 2)) = make_float2(mm, ll);
+    } else if (sees <= a.chunk) {
+      store(q_row(r), d, ox / ll, oy / ll);
     } else {
-      float* const part = a.partial + (qr * a.max_chunks + chunk) * (HD + 2);
+      float* const part = a.partial + (q_row(r) * a.max_chunks + chunk) * (HD + 2);
       __stcg(reinterpret_cast<float2*>(part + 2 + d), make_float2(ox, oy));
       if (d == 0) __stcg(reinterpret_cast<float2*>(part), make_float2(mm, ll));
     }
+  }
+  if constexpr (CLUSTER) {
+    cluster_sync_all();
+    // rows and dims in turn over the cluster's threads; chunks in order
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(own);
+    const int live = (seen_top + a.chunk - 1) / a.chunk;
+    for (int idx = chunk * (KV8_WARPS * 32) + threadIdx.x; idx < rows * (HD / 2); idx += (int)gridDim.z * (KV8_WARPS * 32)) {
+      const int r = idx / (HD / 2), d = idx % (HD / 2) * 2;
+      if (seen0 + (tile * TR + r) / G <= 0) continue;
+      float2 ml[KV8_CLUSTER], v[KV8_CLUSTER];
+      float mm = -INFINITY, ll = 0.f, ox = 0.f, oy = 0.f;
+#pragma unroll
+      for (int c = 0; c < KV8_CLUSTER; ++c)
+        if (c < live) {
+          const uint32_t p = mapa_cluster(base, c) + (uint32_t)r * (HD + 2) * 4;
+          ml[c] = ld_cluster(p);
+          v[c] = ld_cluster(p + 8 + d * 4);
+        }
+#pragma unroll
+      for (int c = 0; c < KV8_CLUSTER; ++c) if (c < live) mm = fmaxf(mm, ml[c].x);
+#pragma unroll
+      for (int c = 0; c < KV8_CLUSTER; ++c)
+        if (c < live) {
+          const float f = ml[c].x == -INFINITY ? 1.f : ex2(ml[c].x - mm);
+          ll += ml[c].y * f;
+          ox += v[c].x * f;
+          oy += v[c].y * f;
+        }
+      store(q_row(r), d, ox / ll, oy / ll);
+    }
+    cluster_sync_all();                            // nobody leaves while its results are read
   }
 }
 
@@ -582,12 +661,24 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) kv8_merge_kernel(const Kv8At
   a.out[qr * HD + d] = f2bf(oo / ll);
 }
 
-// Tokens of a chunk: enough blocks for some waves of three per SM, chunks of 64 to 1024 tokens.
-int kv8_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) {
-  const long long blocks = 12ll * sm_count, items = B * tiles * Hkv, whole = ((long long)max_len + 63) / 64 * 64;
-  if (items >= blocks) return (int)std::min<long long>(whole, 1 << 30);
-  const long long c = ((long long)max_len * items + blocks - 1) / blocks;
-  return (int)std::min(std::min(std::max((c + 63) / 64 * 64, 64ll), 1024ll), whole);
+// Chunks of the kernel for few rows, `slots` blocks being resident at once.
+// Short ones are merged by a cluster of up to eight blocks, all resident: one launch instead of two, which is 2.5 us of the host's time, and
+// no longer on the device (one request of 777 tokens, hd 64: 13 chunks and a second kernel 6.2 us, a cluster of seven 6.0; four of
+// 1000, hd 128: 9.2 and 8.3; but one of 4000, hd 64: 16 chunks 7.2, a cluster of eight 8.2).
+// Otherwise one block a slot for requests as long as the longest one, up to 1.5 where there are many of them, since then they are
+// shorter on the average; chunks of at most 2048 tokens when there are more requests than slots.  A block costs its start and its partial
+// results; too few of them, or a few more than a wave, leave SMs idle at the end.  Device times by chunk, hd 128: 128 requests of
+// 512 to 8192 tokens 1024 198 us, 2048 192, 4096 205; 2 of 100003 and 131072 1024 97, 2432 103, 3456 92, 4096 94; one of 131000 1728 65 (608 blocks for 592 slots), 4096 53; 8 of 4000 to 8192 512
+// 28, 640 28, 768 24, 1024 27, 2048 35; 64 of 512 to 1024 512 30, whole 24; hd 64, 32 of 128 to 4096 512 25, 1408 23, 2048 27.
+struct Chunks { int tokens, clustered; };
+Chunks kv8_chunks(int B, long long items, int slots, int max_len) {
+  auto whole64 = [](long long v) { return (int)std::min((v + 63) / 64 * 64, 1ll << 30); };
+  const long long len = max_len, in_cluster = std::min<long long>(std::max(slots / items, 1ll), KV8_CLUSTER);
+  const int c = whole64((len + in_cluster - 1) / in_cluster);
+  if (c <= 256) return {c, c < len};
+  const long long n = std::max((long long)(slots * std::min(1.0 + (B - 1) / 32.0, 1.5)) / items, 1ll);
+  const long long t = std::max((len + n - 1) / n, std::min(len / 16, 512ll));
+  return {whole64(items >= slots ? std::min(t, 2048ll) : t), 0};
 }
 
 // ... of the kernel for many rows: one CTA to an SM; a chunk of at least 512 tokens, so that what a CTA does around its loop stays small.
@@ -598,14 +689,21 @@ int kv8_flash_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) 
   return (int)std::min(std::max((c + 63) / 64 * 64, 512ll), whole);
 }
 
-struct AttnPlan { int nt, tiles, chunk, chunks; };      // nt 0: the kernel for many rows
+struct AttnPlan { int nt, tiles, chunk, chunks, clustered; };      // nt 0: the kernel for many rows
 AttnPlan attn_plan(int B, int Hq, int Hkv, int max_q, int max_len, int sm_count) {
   AttnPlan p;
   const long long rows = (long long)max_q * (Hq / Hkv);
   p.nt = rows <= 8 ? 1 : rows <= 32 ? 2 : 0;
   const int tile = p.nt ? 8 * p.nt : KV8_FLASH_ROWS;
   p.tiles = (int)((rows + tile - 1) / tile);
-  p.chunk = p.nt ? kv8_chunk(B, p.tiles, Hkv, max_len, sm_count) : kv8_flash_chunk(B, p.tiles, Hkv, max_len, sm_count);
+  p.clustered = 0;
+  if (p.nt) {
+    const Chunks c = kv8_chunks(B, (long long)B * p.tiles * Hkv, (p.nt == 1 ? 4 : 3) * sm_count, max_len);
+    p.chunk = c.tokens;
+    p.clustered = c.clustered;
+  } else {
+    p.chunk = kv8_flash_chunk(B, p.tiles, Hkv, max_len, sm_count);
+  }
   p.chunks = (max_len + p.chunk - 1) / p.chunk;
   return p;
 }
@@ -617,18 +715,37 @@ cudaError_t launch_merge(const Kv8Attn& a, cudaStream_t st) {
 }
 
 template <int HD, int NT>
-cudaError_t launch_attn(const Kv8Attn& a, cudaStream_t st) {
-  const auto kernel = kv8_attn_kernel<HD, NT>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Kv8Geo<HD, NT>::SMEM);
+cudaError_t launch_few(const Kv8Attn& a, bool clustered, cudaStream_t st) {
+  using Geo = Kv8Geo<HD, NT>;
+  const auto kernel = clustered ? kv8_attn_kernel<HD, NT, true> : kv8_attn_kernel<HD, NT, false>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo::SMEM);
   if (e != cudaSuccess) return e;
-  e = launch_pdl(kernel, dim3((unsigned)(a.B * a.tiles), (unsigned)a.Hkv, (unsigned)a.max_chunks), dim3(KV8_WARPS * 32), Kv8Geo<HD, NT>::SMEM, st, a);
-  return e == cudaSuccess ? launch_merge<HD>(a, st) : e;
+  const dim3 grid((unsigned)(a.B * a.tiles), (unsigned)a.Hkv, (unsigned)a.max_chunks);
+  if (!clustered) {
+    e = launch_pdl(kernel, grid, dim3(KV8_WARPS * 32), Geo::SMEM, st, a);
+    return e == cudaSuccess ? launch_merge<HD>(a, st) : e;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(KV8_WARPS * 32);
+  cfg.dynamicSmemBytes = Geo::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = (unsigned)a.max_chunks;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <int HD>
-cudaError_t launch_attn(const Kv8Attn& a, int nt, cudaStream_t st) {
-  if (nt == 1) return launch_attn<HD, 1>(a, st);
-  if (nt == 2) return launch_attn<HD, 2>(a, st);
+cudaError_t launch_attn(const Kv8Attn& a, const AttnPlan& p, cudaStream_t st) {
+  if (p.nt == 1) return launch_few<HD, 1>(a, p.clustered, st);
+  if (p.nt == 2) return launch_few<HD, 2>(a, p.clustered, st);
   const cudaError_t e = launch_kv8_flash(a, HD, st);
   return e == cudaSuccess ? launch_merge<HD>(a, st) : e;
 }
@@ -678,7 +795,7 @@ size_t epara_kv8_attention_scratch_bytes(int device, int B, int T, int Hq, int H
   using namespace epara;
   if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || hd <= 0 || max_q <= 0 || max_len <= 0) return 0;
   const AttnPlan p = attn_plan(B, Hq, Hkv, std::min(max_q, T), max_len, device_sm_count(device));
-  return p.chunks == 1 ? 0 : (size_t)T * Hq * p.chunks * (hd + 2) * sizeof(float);
+  return p.chunks == 1 || p.clustered ? 0 : (size_t)T * Hq * p.chunks * (hd + 2) * sizeof(float);
 }
 
 int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stride, const void* kv8_layer, const float* kv_scales, long long kv_pages,
@@ -702,7 +819,7 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
   a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
   if ((long long)B * a.tiles * Hkv > 0x7fffffffll || (long long)B * a.max_q > 0x7fffffffll || a.max_chunks > 65535) return EPARA_E_UNSUPPORTED;
   if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;
-  const cudaError_t e = hd == 128 ? launch_attn<128>(a, p.nt, (cudaStream_t)cuda_stream) : launch_attn<64>(a, p.nt, (cudaStream_t)cuda_stream);
+  const cudaError_t e = hd == 128 ? launch_attn<128>(a, p, (cudaStream_t)cuda_stream) : launch_attn<64>(a, p, (cudaStream_t)cuda_stream);
   return e == cudaSuccess ? EPARA_OK : EPARA_E_CUDA;
 }
 

@@ -85,9 +85,9 @@ def test_cache_calls_refuse_other_head_sizes(E):
 
 
 def test_attention_asks_for_its_scratch(E):
-    need = E.epara_kv8_attention_scratch_bytes(2, 2, 8, 2, 128, 1, 4096)
+    need = E.epara_kv8_attention_scratch_bytes(2, 2, 8, 2, 128, 1, 131072)
     assert need > 0
-    big = dict(max_len=4096, table_stride=256)
+    big = dict(max_len=131072, table_stride=8192)
     assert _attn(E, scratch_bytes=need - 1, **big) == E.E_RESOURCE
     assert _attn(E, scratch=None, scratch_bytes=need, **big) == E.E_INVALID
     assert _attn(E, scratch=P + 4, scratch_bytes=need, **big) == E.E_INVALID
