@@ -6,11 +6,11 @@
 // relative to the largest of the chunk, are folded into the converted values.  Roles:
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread per query row (at first: that row of Q into shared memory).  A row of S is read
 //                   from tensor memory once and P written over it in fp16.  The running maximum is raised, and O rescaled, only when
-//                   it grows by more than 2^8;
-//   warp 8          issues S_g = Q_g K^T (M 128, N 64) into one of two buffers per tile;
-//   warps 9, 10     issue O_g += P_g V, P as the A operand from tensor memory, V as an MN-major B operand;
-//   warps 11-14     load a page of each step (the next step's while this one's is converted) and write it as the 128-byte-swizzled tiles
-//                   that the MMAs want.  NaN codes of V are taken out (a zero probability times NaN is NaN) and the first key
+//                   it grows by more than 2^8.  The warps of the two tiles on a scheduler take turns at the exponentials, so that one tile's
+//                   scores are read and reduced while the other keeps the special-function unit busy;
+//   warps 8, 9      issue S_g = Q_g K^T (M 128, N 64) into one of two buffers per tile, g = 0 and 1;
+//   warps 10, 11    issue O_g += P_g V, P as the A operand from tensor memory, V as an MN-major B operand;
+//   warps 12-15     request the pages of the next steps, one of each, and write them as the 128-byte-swizzled tiles that the MMAs want.  NaN codes of V are taken out (a zero probability times NaN is NaN) and the first key
 //                   that has one is kept per dim: a row that sees it gets its NaN at the end.
 // With several chunks of keys partial results go to scratch, as in the kernel for few rows, and are merged by the same kernel.
 // Every mbarrier wait is bounded.
@@ -29,7 +29,7 @@ namespace {
 using namespace tc;
 
 constexpr int KF_STEP = 64, KF_TILE = 128;
-constexpr int KF_S_WARP = 8, KF_PV_WARP = 9, KF_CONV_WARP = 11, KF_CONV_WARPS = 4;
+constexpr int KF_S_WARP = 8, KF_PV_WARP = 10, KF_CONV_WARP = 12, KF_CONV_WARPS = 4;
 constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
 constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
 constexpr float KF_RAISE = 8.0f;
@@ -98,6 +98,11 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
   return r;
 }
 
+// The turns of the two softmax warps of a scheduler, a barrier each: a warp waits at its own for the other one's arrival.  They have no limit
+// of their own: a warp that gives up goes on taking and passing its turns.
+__device__ __forceinline__ void turn_wait(int warp) { asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(1 + warp) : "memory"); }
+__device__ __forceinline__ void turn_pass(int warp) { asm volatile("barrier.cta.arrive.aligned %0, 64;" ::"r"(1 + (warp ^ 4)) : "memory"); }
+
 template <int HD>
 __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn a) {
   using Geo = KfGeo<HD>;
@@ -157,7 +162,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     mbar_init(bar(KB_Q), 8);
     for (int i = 0; i < 4; ++i) { mbar_init(bar(KB_S_FULL + i), 1); mbar_init(bar(KB_P_READY + i), 4); mbar_init(bar(KB_PV_DONE + i), 1); }
     for (int s = 0; s < ST; ++s) {
-      mbar_init(bar(KB_K_FULL + s), KF_CONV_WARPS); mbar_init(bar(KB_K_EMPTY + s), 1);
+      mbar_init(bar(KB_K_FULL + s), KF_CONV_WARPS); mbar_init(bar(KB_K_EMPTY + s), n_mt);
       mbar_init(bar(KB_V_FULL + s), KF_CONV_WARPS); mbar_init(bar(KB_V_EMPTY + s), n_mt);
     }
     *abort_flag = 0;
@@ -293,28 +298,28 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       if (lane == 0) mbar_arrive(bar(KB_V_FULL + slot));
     }
     if (!ok) *abort_flag = 1;
-  } else if (warp == KF_S_WARP) {
-    // ------------------------------------------------------------------ issuer of S
+  } else if (warp == KF_S_WARP || warp == KF_S_WARP + 1) {
+    // ------------------------------------------------------------------ issuers of S_t
+    const int t = warp - KF_S_WARP;
     const uint32_t idesc = kf_idesc(KF_STEP);
     if (!mbar_wait<false>(bar(KB_Q), 0u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 25); }
-    for (int j = 0; j < steps && ok; ++j) {
+    const uint64_t dq = make_smem_desc(base + t * Geo::Q_BYTES);
+    for (int j = 0; j < steps && ok && t < n_mt; ++j) {
       const int slot = j % ST, sb = j & 1;
-      if (!mbar_wait<false>(bar(KB_K_FULL + slot), (j / ST) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 26); break; }
-      const uint64_t dk = make_smem_desc(base + Geo::OFF_KV + slot * 2 * Geo::KV_BYTES);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (t >= n_mt) break;
-        // the buffer holds P until the P V of two steps ago is complete
-        if (j >= 2 && !mbar_wait<false>(bar(KB_PV_DONE + 2 * t + sb), ((j >> 1) - 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 27); break; }
-        tc_fence_after();
-        const uint64_t dq = make_smem_desc(base + t * Geo::Q_BYTES);
-        const uint32_t d = tmem_base + KF_S_COL + t * 128 + sb * 64;
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k)
-          mma_f16_elect(d, dq + (uint64_t)((k >> 2) * (KF_Q_HALF >> 4) + (k & 3) * 2), dk + (uint64_t)((k >> 2) * (KF_KV_HALF >> 4) + (k & 3) * 2), idesc, k > 0 ? 1u : 0u);
-        mma_commit_elect(bar(KB_S_FULL + 2 * t + sb));
+      // the buffer holds P until the P V of two steps ago is complete
+      if (!mbar_wait<false>(bar(KB_K_FULL + slot), (j / ST) & 1u, abort_flag) ||
+          (j >= 2 && !mbar_wait<false>(bar(KB_PV_DONE + 2 * t + sb), ((j >> 1) - 1) & 1u, abort_flag))) {
+        ok = false;
+        if (lane == 0) atomicExch(a.status, 26);
+        break;
       }
-      if (!ok) break;
+      tc_fence_after();
+      const uint64_t dk = make_smem_desc(base + Geo::OFF_KV + slot * 2 * Geo::KV_BYTES);
+      const uint32_t d = tmem_base + KF_S_COL + t * 128 + sb * 64;
+#pragma unroll
+      for (int k = 0; k < HD / 16; ++k)
+        mma_f16_elect(d, dq + (uint64_t)((k >> 2) * (KF_Q_HALF >> 4) + (k & 3) * 2), dk + (uint64_t)((k >> 2) * (KF_KV_HALF >> 4) + (k & 3) * 2), idesc, k > 0 ? 1u : 0u);
+      mma_commit_elect(bar(KB_S_FULL + 2 * t + sb));
       mma_commit_elect(bar(KB_K_EMPTY + slot));
     }
     if (!ok) *abort_flag = 1;
@@ -373,7 +378,12 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     const int seen_least = seen0 + warp_r0 / G, seen_most = warp_rows > 0 ? seen0 + (warp_r0 + warp_rows - 1) / G : 0;
     auto k_scale = [&](int i) { const int id = page_id(i); return id >= 0 ? a.scales[(size_t)id * 2 * a.Hkv + kvh] : 0.f; };
     float ks_cur = k_scale(lane), ks_next = k_scale(32 + lane);        // of 8 steps each
-    for (int j = 0; j < steps && g < n_mt; ++j) {
+    // (every turn is taken and passed on once a step, whatever happens; the one before tile 0's first is passed here, tile 1's last one is
+    // not passed on)
+    const bool turns = n_mt == 2;
+    if (turns && g == 1) turn_pass(warp);
+    int j = 0;
+    for (; j < steps && g < n_mt; ++j) {
       const int sb = j & 1, k0 = t_begin + j * KF_STEP;
       if ((j & 7) == 0 && j > 0) { ks_cur = ks_next; ks_next = k_scale((j + 8) * 4 + lane); }
       if (!mbar_wait<false>(bar(KB_S_FULL + 2 * g + sb), (j >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 29); break; }
@@ -381,6 +391,10 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       const uint32_t addr = s_addr + sb * 64;
       if (k0 >= seen_most) {                          // no row of the warp sees any of these keys
         const uint32_t z[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+        if (turns) {
+          turn_wait(warp);
+          if (g == 0 || j + 1 < steps) turn_pass(warp);
+        }
 #pragma unroll
         for (int c = 0; c < 32; c += 8) kf_st8(addr + c, z);
         kf_st_wait();
@@ -428,6 +442,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
             kf_st8(o_addr + c + 8, o + 8);
           }
         }
+        if (turns) turn_wait(warp);
         const uint64_t nm = f2(-m_ref, -m_ref);
         uint64_t la = 0, lb = 0;
 #pragma unroll
@@ -445,6 +460,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
           }
           kf_st8(addr + 8 * p, h);
         }
+        if (turns && (g == 0 || j + 1 < steps)) turn_pass(warp);
         float a0, a1, a2, a3;
         un_f2(la, a0, a1);
         un_f2(lb, a2, a3);
@@ -454,6 +470,13 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(KB_P_READY + 2 * g + sb));
+    }
+    if (!ok) {
+      *abort_flag = 1;
+      for (; turns && j < steps; ++j) {               // (it gave up before this step's turn)
+        turn_wait(warp);
+        if (g == 0 || j + 1 < steps) turn_pass(warp);
+      }
     }
     if (ok && g < n_mt && !mbar_wait<false>(bar(KB_PV_DONE + 2 * g + ((steps - 1) & 1)), ((steps - 1) >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 18); }
     if (!ok) *abort_flag = 1;
