@@ -42,7 +42,7 @@ def build_fastcall(force: bool = False) -> None:
     """The binding works without it (through ctypes): a machine without Python's headers or a C++ compiler that takes the source goes
     without."""
     include = sysconfig.get_paths()["include"]
-    if not os.path.exists(os.path.join(include, "Python.h")) or not (force or _newer(FAST_LIB, [FAST_SRC])):
+    if not os.path.exists(os.path.join(include, "Python.h")) or not (force or _newer(FAST_LIB, [FAST_SRC, os.path.join(HERE, "..", "include", "epara.h")])):
         return
     for old in (FAST_LIB, os.path.join(os.path.dirname(FAST_LIB), "_fastcall.so")):   # of an older source; without an ABI in its name
         if os.path.exists(old):

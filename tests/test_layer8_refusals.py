@@ -93,3 +93,29 @@ def test_attention_asks_for_its_scratch(E):
     assert _attn(E, scratch=P + 4, scratch_bytes=need, **big) == E.E_INVALID
     assert E.epara_kv8_attention_scratch_bytes(2, 2, 8, 2, 128, 1, 64) == 0       # a single chunk needs none
     assert E.epara_kv8_attention_scratch_bytes(2, 2, 7, 2, 128, 1, 64) == 0
+
+
+def test_calls_without_ctypes_take_what_ctypes_takes(E):
+    """The compiled forms of the four calls: the same answers for the same arguments, and Python errors for wrong ones."""
+    fast = pytest.importorskip("paper_2511_00603_b200._fastcall")
+    assert E._norm_i8.__name__ == "epara_rms_norm_i8" and not hasattr(E._gemm_i8, "argtypes") and fast
+    norm = [0, None, P, 0, 64, P, 64, P, 64, P, 1e-5, P, 64, P, 0, 64]
+    gemm = [0, None, P, P, P, P, P, None, 0, 32, 48, 48, 48, 32, 0, P]
+    append = [0, None, P, 256, P, 256, P, P, 10, None, P, P, 4, 0, 0, 2, 128, 1, 64, P]
+    attn = [0, None, P, 1024, P, P, 10, None, P, P, 4, P, 0, 0, 8, 2, 128, 1, 64, None, 0, P]
+    general = [E.lib.epara_rms_norm_i8, E._gemm_i8_ctypes, E.lib.epara_kv8_append, E.lib.epara_kv8_attention]
+    for call, plain, args in zip((E._norm_i8, E._gemm_i8, E._kv8_append, E._kv8_attention), general, (norm, gemm, append, attn)):
+        assert call(*args) == plain(*args) == E.OK
+        for i in range(2, len(args)):
+            pointer = args[i] is None or args[i] == P
+            for other in ((None, P + 1) if pointer else (0.5,) if call is E._norm_i8 and i == 10 else (-7, 1 << 30)):
+                a = args[:i] + [other] + args[i + 1:]
+                if (call is E._norm_i8 and i == 14 or call is E._gemm_i8 and i == 8) and other > 0:
+                    continue                               # (rows to work on: such a call would go on to the GPU)
+                assert call(*a) == plain(*a), (call, i, other)
+        with pytest.raises(TypeError):
+            call(*args[:-1])
+        with pytest.raises(TypeError):
+            call(*args[:2], "7", *args[3:])
+        with pytest.raises(OverflowError):
+            call(1 << 40, *args[1:])
