@@ -376,8 +376,10 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     const int warp_rows = min(rows - g * KF_TILE - (warp & 3) * 32, 32);       // live ones
     const int warp_r0 = r_first + g * KF_TILE + (warp & 3) * 32;
     const int seen_least = seen0 + warp_r0 / G, seen_most = warp_rows > 0 ? seen0 + (warp_r0 + warp_rows - 1) / G : 0;
-    auto k_scale = [&](int i) { const int id = page_id(i); return id >= 0 ? a.scales[(size_t)id * 2 * a.Hkv + kvh] : 0.f; };
-    float ks_cur = k_scale(lane), ks_next = k_scale(32 + lane);        // of 8 steps each
+    // K scales of 32 pages, 8 steps, each: these, the next ones, and the ids of those after them, so that nobody waits for a load
+    auto k_scale = [&](int id) { return id >= 0 ? a.scales[(size_t)id * 2 * a.Hkv + kvh] : 0.f; };
+    float ks_cur = k_scale(page_id(lane)), ks_next = k_scale(page_id(32 + lane));
+    int id_after = page_id(64 + lane);
     // (every turn is taken and passed on once a step, whatever happens; the one before tile 0's first is passed here, tile 1's last one is
     // not passed on)
     const bool turns = n_mt == 2;
@@ -385,7 +387,10 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     int j = 0;
     for (; j < steps && g < n_mt; ++j) {
       const int sb = j & 1, k0 = t_begin + j * KF_STEP;
-      if ((j & 7) == 0 && j > 0) { ks_cur = ks_next; ks_next = k_scale((j + 8) * 4 + lane); }
+      if ((j & 7) == 0 && j > 0) { ks_cur = ks_next; ks_next = k_scale(id_after); id_after = page_id((j + 16) * 4 + lane); }
+      float f[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) f[p] = fmaxf(row_f * __shfl_sync(0xffffffffu, ks_cur, (j & 7) * 4 + p), KV8_TINY_SCALE);
       if (!mbar_wait<false>(bar(KB_S_FULL + 2 * g + sb), (j >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 29); break; }
       tc_fence_after();
       const uint32_t addr = s_addr + sb * 64;
@@ -402,9 +407,6 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
         uint32_t v[64];
         tmem_ld32_nowait(addr, v);
         tmem_ld32_nowait(addr + 32, v + 32);
-        float f[4];
-#pragma unroll
-        for (int p = 0; p < 4; ++p) f[p] = fmaxf(row_f * __shfl_sync(0xffffffffu, ks_cur, (j & 7) * 4 + p), KV8_TINY_SCALE);
         tmem_ld_wait();
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_regs_ready16(v + 16 * c);
