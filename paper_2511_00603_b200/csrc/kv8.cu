@@ -690,10 +690,18 @@ int kv8_flash_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) 
 }
 
 struct AttnPlan { int nt, tiles, chunk, chunks, clustered; };      // nt 0: the kernel for many rows
-AttnPlan attn_plan(int B, int Hq, int Hkv, int max_q, int max_len, int sm_count) {
+// Which kernel: beyond 16 query rows the one for many rows where the work, rows times the tokens of all kv heads, is large enough for its
+// tiles of 128 rows, most of them empty, to cost less than reading the cache again for every 16.  Device times, few rows and many, hd 128: 32
+// requests of 1024 to 2048 tokens, 20 rows 57 and 59 us, 32 rows 68 and 60; 8 of 2048 to 4096, 32 rows 32 and 46, 48 rows 50 and 49, 64 rows 62
+// and 52; one of 16384, 64 rows 37 and 41, 96 rows 46 and 45; one of 1000, 256 rows 19 and 32.  hd 64: 32 of 1024 to 2048, 48 rows 45 and 49, 64
+// rows 60 and 49; 8 of 2048 to 4096, 96 rows 44 and 45; one of 16384, 128 rows 37 and 37.
+// Tiles of 8 rows instead of 16 where contexts are short: 32 requests of up to 2048 tokens, 16 rows, hd 128 41 and 48 us; but 8 of up to 4096
+// 25 and 23.
+AttnPlan attn_plan(int B, int Hq, int Hkv, int hd, int max_q, int max_len, int sm_count) {
   AttnPlan p;
   const long long rows = (long long)max_q * (Hq / Hkv);
-  p.nt = rows <= 8 ? 1 : rows <= 32 ? 2 : 0;
+  const double work = (double)rows * B * Hkv * max_len;
+  p.nt = rows > 16 && work > (hd == 128 ? 12.5e6 : 22e6) ? 0 : rows <= 8 || (rows <= 32 && max_len <= 2048) ? 1 : 2;
   const int tile = p.nt ? 8 * p.nt : KV8_FLASH_ROWS;
   p.tiles = (int)((rows + tile - 1) / tile);
   p.clustered = 0;
@@ -794,7 +802,7 @@ int epara_kv8_append(int device, void* cuda_stream, const void* k, int k_stride,
 size_t epara_kv8_attention_scratch_bytes(int device, int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len) {
   using namespace epara;
   if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || hd <= 0 || max_q <= 0 || max_len <= 0) return 0;
-  const AttnPlan p = attn_plan(B, Hq, Hkv, std::min(max_q, T), max_len, device_sm_count(device));
+  const AttnPlan p = attn_plan(B, Hq, Hkv, hd, std::min(max_q, T), max_len, device_sm_count(device));
   return p.chunks == 1 || p.clustered ? 0 : (size_t)T * Hq * p.chunks * (hd + 2) * sizeof(float);
 }
 
@@ -815,7 +823,7 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
   a.q = (const bf16*)q; a.codes = (const unsigned char*)kv8_layer; a.scales = kv_scales; a.q_rows = q_rows; a.kv_lens = kv_lens; a.tables = tables;
   a.out = (bf16*)out; a.partial = (float*)scratch; a.status = status; a.kv_pages = kv_pages;
   a.q_stride = q_stride; a.table_stride = table_stride; a.B = B; a.T = T; a.Hkv = Hkv; a.G = Hq / Hkv; a.max_q = std::min(max_q, T); a.max_len = max_len;
-  const AttnPlan p = attn_plan(B, Hq, Hkv, a.max_q, max_len, device_sm_count(device));
+  const AttnPlan p = attn_plan(B, Hq, Hkv, hd, a.max_q, max_len, device_sm_count(device));
   a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
   if ((long long)B * a.tiles * Hkv > 0x7fffffffll || (long long)B * a.max_q > 0x7fffffffll || a.max_chunks > 65535) return EPARA_E_UNSUPPORTED;
   if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;

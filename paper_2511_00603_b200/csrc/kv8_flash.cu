@@ -33,6 +33,7 @@ constexpr int KF_S_WARP = 8, KF_PV_WARP = 10, KF_CONV_WARP = 12, KF_CONV_WARPS =
 constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
 constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
 constexpr float KF_RAISE = 8.0f;
+constexpr float KF_HUGE = 4194304.0f;                 // 2^22: the rounding of such a score is up to a quarter of a power of two
 constexpr int KF_SORTED = 512;                        // requests of a call that are put in order
 
 template <int HD>
@@ -382,6 +383,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     int id_after = page_id(64 + lane);
     // (every turn is taken and passed on once a step, whatever happens; the one before tile 0's first is passed here, tile 1's last one is
     // not passed on)
+    bool huge = false;                                // some row's maximum is
     const bool turns = n_mt == 2;
     if (turns && g == 1) turn_pass(warp);
     int j = 0;
@@ -427,9 +429,11 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
         }
         if (j == 0) {
           m_ref = mx == -INFINITY ? 0.f : mx;         // (a row that sees a key of the chunk sees its first one)
+          huge = __any_sync(0xffffffffu, fabsf(m_ref) > KF_HUGE);
         } else if (__any_sync(0xffffffffu, row_live && mx - m_ref > KF_RAISE)) {
           const float m_new = fmaxf(m_ref, mx), r = ex2(m_ref - m_new);
           m_ref = m_new;
+          huge = __any_sync(0xffffffffu, fabsf(m_ref) > KF_HUGE);
           l *= r;
           // every P V up to the step before must be complete
           if (!mbar_wait<false>(bar(KB_PV_DONE + 2 * g + (sb ^ 1)), ((j - 1) >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 30); break; }
@@ -445,7 +449,16 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
           }
         }
         if (turns) turn_wait(warp);
-        const uint64_t nm = f2(-m_ref, -m_ref);
+        float to_add = -m_ref;
+        if (huge) {
+          // (scores of millions: fused, the largest would stand above or below its own rounded maximum; product and difference apart)
+#pragma unroll
+          for (int i = 0; i < 64; ++i) v[i] = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(v[i]), f[i >> 4]), -m_ref));
+#pragma unroll
+          for (int p = 0; p < 4; ++p) f[p] = 1.f;
+          to_add = 0.f;
+        }
+        const uint64_t nm = f2(to_add, to_add);
         uint64_t la = 0, lb = 0;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {

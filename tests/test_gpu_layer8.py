@@ -229,12 +229,17 @@ def test_gemm_sums_are_exact_whatever_the_kernel(E):
 
 # ------------------------------------------------------------------------------------------------ cache
 class Cache:
-    def __init__(self, B, max_len, Hkv, hd, seed, spare=3, fill="random"):
+    """max_len: what the calls are told, which decides about kernels and chunks; used: tokens that there are pages for (the tables name
+    none behind them)."""
+
+    def __init__(self, B, max_len, Hkv, hd, seed, spare=3, fill="random", used=None):
         g = _gen(seed)
         self.B, self.max_len, self.Hkv, self.hd = B, max_len, Hkv, hd
         self.width = (max_len + 15) // 16
-        self.pages = B * self.width + spare
-        self.tables = torch.randperm(self.pages, generator=g, device="cuda")[:B * self.width].to(torch.int32).view(B, self.width)
+        used = (min(used or max_len, max_len) + 15) // 16
+        self.pages = B * used + spare
+        self.tables = torch.full((B, self.width), -1, dtype=torch.int32, device="cuda")
+        self.tables[:, :used] = torch.randperm(self.pages, generator=g, device="cuda")[:B * used].to(torch.int32).view(B, used)
         shape = (self.pages, 2, Hkv, 16, hd)
         if fill == "random":
             self.codes = (torch.randn(shape, generator=g, device="cuda") * 60).clamp(-448, 448).to(torch.float8_e4m3fn)
@@ -247,6 +252,13 @@ class Cache:
         page = self.tables[b, : (n + 15) // 16].long()
         kv = self.codes.view(torch.uint8)[page].view(torch.float8_e4m3fn).to(F64) * self.scales[page].to(F64)[..., None, None]
         return kv.permute(1, 2, 0, 3, 4).reshape(2, self.Hkv, -1, self.hd)[:, :, :n]
+
+
+class Part:
+    """One request of a cache."""
+
+    def __init__(self, c, b):
+        self.Hkv, self.hd, self.values = c.Hkv, c.hd, lambda _, n: c.values(b, n)
 
 
 def _rows(ns):
@@ -327,8 +339,9 @@ def test_attention_one_token(E, hd, Hkv, G):
     ([1, 2, 3, 0, 4], [1, 2, 3, 9, 500]), ([5, 16, 17, 1], [5, 16, 400, 77]), ([33, 0, 64, 100], [33, 1, 1000, 129]), ([130, 7, 257], [130, 900, 700]),
     ([600, 31], [1090, 600]), ([40, 4], [17, 2]),          # (fewer tokens than new rows: the first rows see none)
 ])
-def test_attention_several_tokens(E, hd, Hkv, G, ns, lens):
-    c = Cache(len(ns), 1100, Hkv, hd, sum(ns) + G)
+@pytest.mark.parametrize("max_len", [1100, 4000, 1 << 20])     # the last one: the kernel for many rows wherever there are more than 16
+def test_attention_several_tokens(E, hd, Hkv, G, ns, lens, max_len):
+    c = Cache(len(ns), max_len, Hkv, hd, sum(ns) + G, used=1100)
     T = sum(ns)
     q = torch.randn((T + 3, Hkv * G * hd), generator=_gen(T), device="cuda").to(torch.bfloat16)
     out, st = _attend(E, c, q, lens, ns, G)
@@ -340,7 +353,7 @@ def test_attention_several_tokens(E, hd, Hkv, G, ns, lens):
 @pytest.mark.parametrize("hd", [64, 128])
 def test_attention_long_context(E, hd):
     c = Cache(2, 40000, 2, hd, 3)
-    for ns, lens in (([1, 1], [40000, 33333]), ([20, 3], [39999, 20])):
+    for ns, lens in (([1, 1], [40000, 33333]), ([20, 3], [39999, 20]), ([70, 40], [40000, 31000])):
         q = (2 * torch.randn((sum(ns), 8 * hd), generator=_gen(4), device="cuda")).to(torch.bfloat16)
         out, _ = _attend(E, c, q, lens, ns, 4)
         _check_attention(c, q, lens, ns, 4, out)
@@ -348,10 +361,11 @@ def test_attention_long_context(E, hd):
 
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("ns", [[1, 1, 1], [5, 1, 40], [70, 200, 33]])
-def test_attention_does_not_see_what_stands_behind(E, hd, ns):
+@pytest.mark.parametrize("max_len", [320, 1 << 20])
+def test_attention_does_not_see_what_stands_behind(E, hd, ns, max_len):
     """Slots behind the length, tokens behind a row's own, pages of nobody: NaN in all of them; and large and small scales side by side."""
     lens = [77, 300, 223]
-    c = Cache(3, 320, 2, hd, 8)
+    c = Cache(3, max_len, 2, hd, 8, used=320)
     codes = c.codes.view(torch.uint8)
     used = torch.zeros((c.pages, 16), dtype=torch.bool, device="cuda")
     for b, L in enumerate(lens):
@@ -374,16 +388,19 @@ def test_attention_does_not_see_what_stands_behind(E, hd, ns):
     _check_attention(c, q, lens, ns, 4, out, "NaN tokens")
 
 
-def test_attention_extreme_queries(E):
-    c = Cache(4, 200, 1, 64, 6)
-    lens, ns = [200, 150, 3, 90], [1, 1, 1, 1]
-    q = torch.randn((4, 4 * 64), generator=_gen(1), device="cuda")
-    q[0] *= 2.0 ** 60
-    q[1] *= 2.0 ** -60
-    q[2] *= 300
-    q[3, 3] = float("inf")
-    q = q.to(torch.bfloat16)
+@pytest.mark.parametrize("many", [0, 30])                  # rows before the last one of each request: 30 reach the kernel for many rows
+def test_attention_extreme_queries(E, many):
+    c = Cache(4, 1 << 20 if many else 200, 1, 64, 6, used=200)
+    lens, ns = [200, 150, 33, 90], [1 + many] * 4
+    q = torch.randn((4, 1 + many, 4 * 64), generator=_gen(1), device="cuda")
+    q[0, -1] *= 2.0 ** 60
+    q[1, -1] *= 2.0 ** -60
+    q[2, -1] *= 300
+    q[3, -1, 3] = float("inf")
+    q = q.to(torch.bfloat16).view(4 * (1 + many), 4 * 64)
     out, _ = _attend(E, c, q, lens, ns, 4)
+    last = torch.arange(4, device="cuda") * (1 + many) + many
+    q, out = q[last], out[last]
     K, V = c.values(0, 200)
     t = torch.einsum("gd,hld->gl", q[0].to(F64).view(4, 64), K)
     hit = V[0][t.argmax(1)]                                # scores of 2^60: the largest takes all
@@ -394,8 +411,9 @@ def test_attention_extreme_queries(E):
     assert torch.isnan(out[3, :64].float()).all() and torch.isfinite(out[3, 64:].float()).all()
 
 
-def test_attention_strides_and_alignment(E):
-    c, lens, ns = Cache(3, 600, 2, 128, 9), [600, 17, 345], [1, 30, 2]
+@pytest.mark.parametrize("max_len", [600, 1 << 20])
+def test_attention_strides_and_alignment(E, max_len):
+    c, lens, ns = Cache(3, max_len, 2, 128, 9, used=600), [600, 17, 345], [1, 30, 2]
     wide = torch.randn((33, 8 * 128 + 512), generator=_gen(3), device="cuda").to(torch.bfloat16)      # q inside a QKV row
     flat = torch.full((33 * 1024 + 5,), 55.0, dtype=torch.bfloat16, device="cuda")
     for off in (0, 1, 2, 5):
@@ -423,7 +441,9 @@ def test_bad_pages_rows_and_lengths_are_reported_and_skipped(E):
     q = torch.randn((9, 8 * 64), generator=_gen(2), device="cuda").to(torch.bfloat16)
     out, st = _attend(E, c, q, lens, [1, 7, 1], 4, max_q=3)
     full, _ = _attend(E, c, q, lens, [1, 7, 1], 4)
-    assert st.item() == E.ERR_ROWS and torch.equal(out[:4], full[:4]) and (out[4:8] == 55).all() and torch.equal(out[8], full[8])
+    assert st.item() == E.ERR_ROWS and (out[4:8] == 55).all() and torch.equal(out[8], full[8])
+    _check_attention(c, q[:1], lens[:1], [1], 4, out[:1])
+    _check_attention(Part(c, 1), q[1:4], [lens[1] - 4], [3], 4, out[1:4])
     # prefix sums that leave the tensor are clamped to it
     out, st = _attend(E, c, q, lens, [1], 4, q_rows=_int([-5, 1, 4, 10 ** 9]), max_q=9)
     assert (out.float() != 55).any(1).all()
@@ -690,3 +710,21 @@ def test_an_8_bit_cache_beside_the_bf16_one(E):
     # V off by 2^-4 of itself at most; K by as much: a score by at most 2^-4 sum |q k| / sqrt(hd), in practice its root
     rel = ((out.to(F64) - ref.to(F64)).norm() / ref.to(F64).norm()).item()
     assert rel < 2.0 ** -4 * 3, rel
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_many_rows_bad_pages_and_rows_beyond_max_q(E, hd):
+    """The kernel for many rows: a page outside the pool is reported and not read, the other requests are as they were; rows beyond max_q stay."""
+    c = Cache(3, 1 << 20, 2, hd, 2, used=300)
+    lens, ns = [300, 150, 220], [40, 90, 25]
+    q = torch.randn((155, 8 * hd), generator=_gen(2), device="cuda").to(torch.bfloat16)
+    good, st = _attend(E, c, q, lens, ns, 4)
+    _check_attention(c, q, lens, ns, 4, good)
+    keep = c.tables.clone()
+    c.tables[1, 2], c.tables[1, 5] = c.pages, -3
+    out, bad = _attend(E, c, q, lens, ns, 4)
+    assert st.item() == 0 and bad.item() == E.ERR_PAGE_ATTEND and torch.equal(out[:40], good[:40]) and torch.equal(out[130:], good[130:])
+    c.tables.copy_(keep)
+    out, st = _attend(E, c, q, lens, ns, 4, max_q=41)
+    assert st.item() == E.ERR_ROWS and torch.equal(out[:40], good[:40]) and (out[81:130] == 55).all() and torch.equal(out[130:], good[130:])
+    _check_attention(Part(c, 1), q[40:81], [lens[1] - 49], [41], 4, out[40:81])
