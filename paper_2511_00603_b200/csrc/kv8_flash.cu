@@ -33,7 +33,6 @@ constexpr int KF_S_WARP = 8, KF_PV_WARP = 10, KF_CONV_WARP = 12, KF_CONV_WARPS =
 constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
 constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
 constexpr float KF_RAISE = 8.0f;
-constexpr float KF_HUGE = 4194304.0f;                 // 2^22: the rounding of such a score is up to a quarter of a power of two
 constexpr int KF_SORTED = 512;                        // requests of a call that are put in order
 
 template <int HD>
@@ -103,6 +102,13 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
 // of their own: a warp that gives up goes on taking and passing its turns.
 __device__ __forceinline__ void turn_wait(int warp) { asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(1 + warp) : "memory"); }
 __device__ __forceinline__ void turn_pass(int warp) { asm volatile("barrier.cta.arrive.aligned %0, 64;" ::"r"(1 + (warp ^ 4)) : "memory"); }
+
+// The exponents are score x factor - maximum, fused, and the maximum is rounded: beyond 2^27 the largest score would stand more than 2^4
+// above or below its own maximum.  A row with such a maximum has score and maximum scaled down to 2^26 by a power of two: neighbouring fp32
+// scores are then still 4 apart, equal ones have equal weights and others next to none, as they should.
+__device__ __forceinline__ float scale_down(float m) {
+  return fabsf(m) > 134217728.f ? __uint_as_float((280u - (__float_as_uint(fabsf(m)) >> 23)) << 23) : 1.f;
+}
 
 template <int HD>
 __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn a) {
@@ -383,7 +389,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     int id_after = page_id(64 + lane);
     // (every turn is taken and passed on once a step, whatever happens; the one before tile 0's first is passed here, tile 1's last one is
     // not passed on)
-    bool huge = false;                                // some row's maximum is
+    float down = 1.f;
     const bool turns = n_mt == 2;
     if (turns && g == 1) turn_pass(warp);
     int j = 0;
@@ -429,11 +435,11 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
         }
         if (j == 0) {
           m_ref = mx == -INFINITY ? 0.f : mx;         // (a row that sees a key of the chunk sees its first one)
-          huge = __any_sync(0xffffffffu, fabsf(m_ref) > KF_HUGE);
+          down = scale_down(m_ref);
         } else if (__any_sync(0xffffffffu, row_live && mx - m_ref > KF_RAISE)) {
           const float m_new = fmaxf(m_ref, mx), r = ex2(m_ref - m_new);
           m_ref = m_new;
-          huge = __any_sync(0xffffffffu, fabsf(m_ref) > KF_HUGE);
+          down = scale_down(m_ref);
           l *= r;
           // every P V up to the step before must be complete
           if (!mbar_wait<false>(bar(KB_PV_DONE + 2 * g + (sb ^ 1)), ((j - 1) >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 30); break; }
@@ -449,20 +455,12 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
           }
         }
         if (turns) turn_wait(warp);
-        float to_add = -m_ref;
-        if (huge) {
-          // (scores of millions: fused, the largest would stand above or below its own rounded maximum; product and difference apart)
-#pragma unroll
-          for (int i = 0; i < 64; ++i) v[i] = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(v[i]), f[i >> 4]), -m_ref));
-#pragma unroll
-          for (int p = 0; p < 4; ++p) f[p] = 1.f;
-          to_add = 0.f;
-        }
-        const uint64_t nm = f2(to_add, to_add);
+        const uint64_t nm = f2(-m_ref * down, -m_ref * down);
         uint64_t la = 0, lb = 0;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
-          const uint64_t ff = f2(f[p], f[p]);
+          const float fd = fmaxf(f[p] * down, KV8_TINY_SCALE);             // (not zero: a masked score times zero is NaN)
+          const uint64_t ff = f2(fd, fd);
           uint32_t h[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
