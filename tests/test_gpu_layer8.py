@@ -59,7 +59,7 @@ def _check_norm(x, r, gain, q, s, r_out, eps=1e-5):
 
 
 @pytest.mark.parametrize("rows", [1, 5, 300])
-@pytest.mark.parametrize("d", [1, 7, 64, 200, 1000, 1111, 2048, 4096, 8200, 16384, 16400, 20001])
+@pytest.mark.parametrize("d", [1, 7, 64, 100, 200, 1000, 1111, 1112, 2048, 4092, 4096, 4097, 8200, 8205, 16384, 16400, 20001])
 @pytest.mark.parametrize("x_type,resid", [("bf16", True), ("bf16", False), ("f32", True)])
 def test_norm(E, rows, d, x_type, resid):
     g = _gen(rows * 31 + d)
@@ -113,6 +113,9 @@ def test_norm_of_zeros_and_of_what_is_not_finite(E, d):
     x = torch.full((1, d), 1e-41, device="cuda")           # subnormal: the scale does not vanish
     E.epara_rms_norm_i8(x, None, q[:1], s[:1], _st())
     assert s[0] == 2.0 ** -126 and (q[0] == 0).all()
+    x.fill_(2e-39)                                         # 316 times that, the norm's 1 / sqrt(eps), over the smallest scale: 54
+    E.epara_rms_norm_i8(x, gain, q[:1], s[:1], _st())
+    assert s[0] == 2.0 ** -126 and (q[0] == round(2e-39 * 1e-5 ** -0.5 * 2.0 ** 126)).all()
 
 
 # ------------------------------------------------------------------------------------------------ product
