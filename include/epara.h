@@ -392,7 +392,7 @@ size_t epara_static_scratch_bytes(void);
  * Calls in the order of a layer: epara_rms_norm_i8 (activations to int8), epara_gemm_i8 (Wqkv), epara_kv8_append, epara_kv8_attention,
  * epara_rms_norm_i8 without gain (quantises the attention's output), epara_gemm_i8 (Wo into the residual stream), and the same pair of
  * calls around the MLP.  They launch kernels on the given stream and nothing else: no allocation, no copy, no synchronisation, so
- * they can be captured into CUDA graphs.  Every argument may be what the call before wrote.
+ * they can be captured into CUDA graphs.  Every argument may be what the call before wrote.  `device` is current during the call only.
  * `status`: device int32 which the caller clears and a kernel sets to a code of epara_output.device_error when it finds something wrong
  * (the access is skipped, the affected outputs must not be used); no call clears it, calls may share it. */
 enum { EPARA_T_BF16 = 0, EPARA_T_F32 = 1 };
@@ -401,14 +401,14 @@ enum { EPARA_T_BF16 = 0, EPARA_T_F32 = 1 };
  *   h = x + resid;  y = h * gain / sqrt(mean(h^2) + eps);  scales[row] = max(max|y| / 127, 2^-126);  q = round(y / scale).
  * x [rows, x_stride] bf16 or fp32 (x_type); resid fp32 or NULL; resid_out receives h in fp32 (NULL: not written; may be resid itself);
  * gain bf16 [d], NULL: no norm, y = h; q int8 [rows, q_stride]; strides in elements.  A row in which h, or the sum of its squares in fp32, is
- * not finite gets a NaN scale and zero codes.  Any d, strides and alignment; vectors are used where d, the strides and the pointers are
+ * not finite gets a NaN scale and zero codes.  Any d up to 2^30, strides and alignment; vectors are used where d, the strides and the pointers are
  * multiples of 8 elements / 16 bytes. */
 int epara_rms_norm_i8(int device, void* cuda_stream, const void* x, int x_type, long long x_stride, const float* resid, long long resid_stride,
                       float* resid_out, long long resid_out_stride, const void* gain, float eps, signed char* q, long long q_stride, float* scales,
                       int rows, int d);
 
 /* C = epilogue((A W^T) * a_scale[m] * w_scale[n] + bias): int8 operands, exact int32 sums, epilogues as epara_grouped_gemm.
- * K at most EPARA_GEMM_I8_MAX_K (no sum passes 31 bits); beyond it UNSUPPORTED.  Rows of A and W may be read up to the next multiple of
+ * K at most EPARA_GEMM_I8_MAX_K (no sum passes 31 bits) and at most 2^30 tiles of 128 x 128 outputs; beyond it UNSUPPORTED.  Rows of A and W may be read up to the next multiple of
  * 16 values, what stands behind K is ignored.  Nothing outside C's N (SwiGLU N / 2) columns is written.  A bounded wait that ran out leaves
  * 51..59 in *status. */
 #define EPARA_GEMM_I8_MAX_K 131071
@@ -431,7 +431,7 @@ int epara_gemm_i8(int device, void* cuda_stream, const epara_gemm_i8_problem* pr
  * Rows: T rows of q, k, v belong to B requests, request b to rows q_rows[b] .. q_rows[b+1] - 1 (device int32 [B + 1], not decreasing), at most
  * max_q of them (more: 103 in *status, the rows beyond are left out); q_rows NULL: one row each, T = B, max_q = 1.  kv_lens [B]: tokens
  * of the request INCLUDING its new ones, so new token i of n stands at position kv_lens[b] - n + i and attends to positions up to its own.
- * tables int32 [B, table_stride], table_stride >= ceil(max_len / 16).
+ * tables int32 [B, table_stride], table_stride >= ceil(max_len / 16).  max_len at most 2^30, else UNSUPPORTED.
  *
  * epara_kv8_append writes k, v (bf16 [T, k_stride], [T, v_stride], kv head h at column h*hd; keys already rotated) to their slots, in pages
  * that no other request of the call appends to.  The scale of a (page, K|V, head) becomes the smallest power of two that brings
@@ -445,7 +445,8 @@ int epara_kv8_append(int device, void* cuda_stream, const void* k, int k_stride,
 
 /* Attention over such a layer, one or several new tokens per request, causal, GQA: q bf16 [T, q_stride] (head h at column h*hd), out bf16
  * [T, Hq*hd] at any 2-byte boundary.  kv_lens outside [0, max_len] are clamped.  A row that attends to no token, and rows that belong to no
- * request, are left unwritten.  A page id outside [0, kv_pages) is read as absent and leaves 102 in *status.
+ * request, are left unwritten.  A page id outside [0, kv_pages) is never dereferenced and leaves 102 in *status: the
+ * request's outputs must not be used, the others are as they should be.
  * scratch: 16-byte aligned, epara_kv8_attention_scratch_bytes() with the same arguments (0: may be NULL); it holds partial results of the
  * call, nothing has to be cleared, calls that may overlap on the GPU need one each. */
 int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stride, const void* kv8_layer, const float* kv_scales, long long kv_pages,

@@ -591,16 +591,18 @@ extern "C" int epara_gemm_i8(int device, void* cuda_stream, const epara_gemm_i8_
   using namespace epara;
   if (!p || !status || !aligned(status, 4)) return EPARA_E_INVALID;
   const epara_gemm_i8_problem& q = *p;
-  if (!q.A || !q.W || !q.C || !q.a_scale || !q.w_scale || q.M < 0 || q.N <= 0 || q.K <= 0) return EPARA_E_INVALID;
-  if (q.K > EPARA_GEMM_I8_MAX_K) return EPARA_E_UNSUPPORTED;
+  if (q.M < 0 || q.N <= 0 || q.K <= 0) return EPARA_E_INVALID;
+  if (q.M == 0) return EPARA_OK;                   // (whose tensors may have no address)
+  if (!q.A || !q.W || !q.C || !q.a_scale || !q.w_scale) return EPARA_E_INVALID;
+  if (q.K > EPARA_GEMM_I8_MAX_K || ((long long)q.M + 127) / 128 * (((long long)q.N + 127) / 128) > 1 << 30) return EPARA_E_UNSUPPORTED;
   if (q.lda % 16 || q.ldw % 16 || q.lda < q.K || q.ldw < q.K) return EPARA_E_INVALID;
   const bool f32 = (q.epilogue & EPARA_EPI_RESID_F32) != 0, swi = (q.epilogue & EPARA_EPI_SWIGLU) != 0;
   if (!aligned(q.A, 16) || !aligned(q.W, 16) || !aligned(q.C, 16) || !aligned(q.a_scale, 16) || !aligned(q.w_scale, 16)) return EPARA_E_INVALID;
   if ((q.epilogue & EPARA_EPI_BIAS) && (!q.bias || !aligned(q.bias, 16))) return EPARA_E_INVALID;
   if ((q.epilogue & ~(EPARA_EPI_BIAS | EPARA_EPI_GELU | EPARA_EPI_SWIGLU | EPARA_EPI_RESID_F32)) || (swi && (q.N % 2 || f32))) return EPARA_E_INVALID;
   if (q.ldc < (swi ? q.N / 2 : q.N)) return EPARA_E_INVALID;
-  if (q.M == 0) return EPARA_OK;
-  if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;
+  const DeviceScope scope(device);
+  if (!scope.ok) return EPARA_E_CUDA;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const int sm = device_sm_count(device);
   const I8Plan plan = i8_plan(q.M, q.N, q.K, sm);

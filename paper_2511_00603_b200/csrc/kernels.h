@@ -109,6 +109,20 @@ int attn_encoder_q_blocks(int T);
 int device_sm_count(int device);
 void* tensor_map_encoder();              // the driver's cuTensorMapEncodeTiled, null where there is none
 
+// Makes a device current for the length of a call.
+struct DeviceScope {
+  int before = -1;
+  bool ok;
+  explicit DeviceScope(int device) {
+    ok = cudaGetDevice(&before) == cudaSuccess && (before == device || cudaSetDevice(device) == cudaSuccess);
+    if (!ok) (void)cudaGetLastError();
+    if (!ok || before == device) before = -1;
+  }
+  ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
+  DeviceScope(const DeviceScope&) = delete;
+  DeviceScope& operator=(const DeviceScope&) = delete;
+};
+
 // 8-bit KV cache (kv8.cu): one call's arguments, passed to the kernels by value.
 struct Kv8Append {
   const bf16* k;

@@ -763,10 +763,10 @@ inline bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr
 // What both calls ask of the cache, the tables and the rows.
 int check_cache(const void* codes, const float* scales, long long kv_pages, const int32_t* q_rows, const int32_t* kv_lens, const int32_t* tables,
                 int table_stride, int B, int T, int Hkv, int hd, int max_q, int max_len, const int* status) {
-  if (!codes || !scales || !kv_lens || !tables || !status || kv_pages <= 0 || B < 0 || T < 0 || Hkv <= 0 || hd <= 0 || max_q <= 0 || max_len <= 0) return EPARA_E_INVALID;
+  if (!codes || !scales || !kv_lens || !tables || !status || kv_pages <= 0) return EPARA_E_INVALID;
   if (!aligned(codes, 16) || !aligned(scales, 4) || !aligned(q_rows, 4) || !aligned(kv_lens, 4) || !aligned(tables, 4) || !aligned(status, 4)) return EPARA_E_INVALID;
   if (table_stride < ((long long)max_len + PAGE - 1) / PAGE || (!q_rows && max_q != 1) || (!q_rows && T != B)) return EPARA_E_INVALID;
-  if (hd != 64 && hd != 128) return EPARA_E_UNSUPPORTED;
+  if ((hd != 64 && hd != 128) || max_len > 1 << 30) return EPARA_E_UNSUPPORTED;
   if (Hkv > 65535) return EPARA_E_UNSUPPORTED;
   return EPARA_OK;
 }
@@ -780,11 +780,12 @@ int epara_kv8_append(int device, void* cuda_stream, const void* k, int k_stride,
                      long long kv_pages, const int32_t* q_rows, const int32_t* kv_lens, const int32_t* tables, int table_stride, int B, int T,
                      int Hkv, int hd, int max_q, int max_len, int* status) {
   using namespace epara;
+  if (B < 0 || T < 0 || Hkv <= 0 || hd <= 0 || max_q <= 0 || max_len <= 0) return EPARA_E_INVALID;
+  if (B == 0 || T == 0) return EPARA_OK;           // (whose tensors may have no address)
   if (!k || !v || !aligned(k, 16) || !aligned(v, 16) || k_stride % 8 || v_stride % 8) return EPARA_E_INVALID;
   const int c = check_cache(kv8_layer, kv_scales, kv_pages, q_rows, kv_lens, tables, table_stride, B, T, Hkv, hd, max_q, max_len, status);
   if (c != EPARA_OK) return c;
   if ((long long)k_stride < (long long)Hkv * hd || (long long)v_stride < (long long)Hkv * hd) return EPARA_E_INVALID;
-  if (B == 0 || T == 0) return EPARA_OK;
   Kv8Append a;
   a.k = (const bf16*)k; a.v = (const bf16*)v; a.codes = (unsigned char*)kv8_layer; a.scales = kv_scales;
   a.q_rows = q_rows; a.kv_lens = kv_lens; a.tables = tables; a.status = status; a.kv_pages = kv_pages;
@@ -792,7 +793,8 @@ int epara_kv8_append(int device, void* cuda_stream, const void* k, int k_stride,
   a.max_q = std::min(max_q, T);
   a.pages_per_request = (std::min(a.max_q, max_len) + PAGE - 2) / PAGE + 1;
   if ((long long)B * a.pages_per_request > 0x7fffffffll) return EPARA_E_UNSUPPORTED;
-  if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;
+  const DeviceScope scope(device);
+  if (!scope.ok) return EPARA_E_CUDA;
   const dim3 grid((unsigned)(B * a.pages_per_request), (unsigned)((2 * Hkv + APPEND_WARPS - 1) / APPEND_WARPS));
   const cudaError_t e = hd == 128 ? launch_pdl(kv8_append_kernel<128>, grid, dim3(APPEND_WARPS * 32), 0, (cudaStream_t)cuda_stream, a)
                                   : launch_pdl(kv8_append_kernel<64>, grid, dim3(APPEND_WARPS * 32), 0, (cudaStream_t)cuda_stream, a);
@@ -810,11 +812,12 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
                         const int32_t* q_rows, const int32_t* kv_lens, const int32_t* tables, int table_stride, void* out, int B, int T, int Hq, int Hkv,
                         int hd, int max_q, int max_len, void* scratch, size_t scratch_bytes, int* status) {
   using namespace epara;
-  if (!q || !out || Hq <= 0 || Hkv <= 0 || Hq % Hkv || !aligned(q, 16) || q_stride % 8 || !aligned(out, 2)) return EPARA_E_INVALID;
+  if (B < 0 || T < 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || hd <= 0 || max_q <= 0 || max_len <= 0) return EPARA_E_INVALID;
+  if (B == 0 || T == 0) return EPARA_OK;           // (whose tensors may have no address)
+  if (!q || !out || !aligned(q, 16) || q_stride % 8 || !aligned(out, 2)) return EPARA_E_INVALID;
   const int c = check_cache(kv8_layer, kv_scales, kv_pages, q_rows, kv_lens, tables, table_stride, B, T, Hkv, hd, max_q, max_len, status);
   if (c != EPARA_OK) return c;
   if ((long long)q_stride < (long long)Hq * hd) return EPARA_E_INVALID;
-  if (B == 0 || T == 0) return EPARA_OK;
   if (Hq > 65535) return EPARA_E_UNSUPPORTED;
   const size_t need = epara_kv8_attention_scratch_bytes(device, B, T, Hq, Hkv, hd, max_q, max_len);
   if (scratch_bytes < need) return EPARA_E_RESOURCE;
@@ -826,7 +829,8 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
   const AttnPlan p = attn_plan(B, Hq, Hkv, hd, a.max_q, max_len, device_sm_count(device));
   a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
   if ((long long)B * a.tiles * Hkv > 0x7fffffffll || (long long)B * a.max_q > 0x7fffffffll || a.max_chunks > 65535) return EPARA_E_UNSUPPORTED;
-  if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;
+  const DeviceScope scope(device);
+  if (!scope.ok) return EPARA_E_CUDA;
   const cudaError_t e = hd == 128 ? launch_attn<128>(a, p, (cudaStream_t)cuda_stream) : launch_attn<64>(a, p, (cudaStream_t)cuda_stream);
   return e == cudaSuccess ? EPARA_OK : EPARA_E_CUDA;
 }

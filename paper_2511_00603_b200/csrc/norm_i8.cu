@@ -340,13 +340,15 @@ extern "C" int epara_rms_norm_i8(int device, void* cuda_stream, const void* x, i
                                  long long resid_stride, float* resid_out, long long resid_out_stride, const void* gain, float eps,
                                  signed char* q, long long q_stride, float* scales, int rows, int d) {
   using namespace epara;
-  if (!x || !q || !scales || rows < 0 || d <= 0 || (x_type != EPARA_T_BF16 && x_type != EPARA_T_F32)) return EPARA_E_INVALID;
+  if (rows < 0 || d <= 0 || (x_type != EPARA_T_BF16 && x_type != EPARA_T_F32) || !(eps >= 0.f)) return EPARA_E_INVALID;
+  if (d > 1 << 30) return EPARA_E_UNSUPPORTED;
+  if (rows == 0) return EPARA_OK;                  // (whose tensors may have no address)
+  if (!x || !q || !scales) return EPARA_E_INVALID;
   if (x_stride < d || q_stride < d || (resid && resid_stride < d) || (resid_out && (!resid || resid_out_stride < d))) return EPARA_E_INVALID;
   const bool f32 = x_type == EPARA_T_F32;
   if (!aligned(x, f32 ? 4 : 2) || !aligned(scales, 4) || !aligned(resid, 4) || !aligned(resid_out, 4) || !aligned(gain, 2)) return EPARA_E_INVALID;
-  if (!(eps >= 0.f)) return EPARA_E_INVALID;
-  if (rows == 0) return EPARA_OK;
-  if (cudaSetDevice(device) != cudaSuccess) return EPARA_E_CUDA;
+  const DeviceScope scope(device);
+  if (!scope.ok) return EPARA_E_CUDA;
   NormI8 a;
   a.x = x; a.resid = resid; a.resid_out = resid_out; a.gain = (const bf16*)gain; a.q = (int8_t*)q; a.scales = scales;
   a.x_stride = x_stride; a.resid_stride = resid_stride; a.out_stride = resid_out_stride; a.q_stride = q_stride;

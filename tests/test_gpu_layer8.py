@@ -731,3 +731,55 @@ def test_many_rows_bad_pages_and_rows_beyond_max_q(E, hd):
     out, st = _attend(E, c, q, lens, ns, 4, max_q=41)
     assert st.item() == E.ERR_ROWS and torch.equal(out[:40], good[:40]) and (out[81:130] == 55).all() and torch.equal(out[130:], good[130:])
     _check_attention(Part(c, 1), q[40:81], [lens[1] - 49], [41], 4, out[40:81])
+
+
+@pytest.mark.parametrize("M", [3, 100, 700])
+def test_a_call_reads_what_the_call_before_wrote(E, M):
+    """Weights quantised on the stream right before the product that reads them, in the same buffers again and again; the result quantised in turn."""
+    N, K, st = 640, 1024, _status()
+    A = torch.randint(-127, 128, (M, K), generator=_gen(1), device="cuda", dtype=torch.int8)
+    sa = torch.rand(M, generator=_gen(2), device="cuda")
+    W8, ws, C = torch.empty((N, K), dtype=torch.int8, device="cuda"), torch.empty(N, device="cuda"), torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    C8, cs = torch.empty((M, N), dtype=torch.int8, device="cuda"), torch.empty(M, device="cuda")
+    Ws = [torch.randn((N, K), generator=_gen(9 + i), device="cuda").to(torch.bfloat16) for i in range(8)]
+
+    def run(W, wait):
+        for call in (lambda: E.epara_rms_norm_i8(W, None, W8, ws, _st()),
+                     lambda: E.epara_gemm_i8(dict(A=A, W=W8, a_scale=sa, w_scale=ws, C=C, M=M, N=N, K=K), _st(), st),
+                     lambda: E.epara_rms_norm_i8(C, None, C8, cs, _st())):
+            call()
+            if wait:
+                torch.cuda.synchronize()
+        return C.clone(), C8.clone(), cs.clone()
+
+    want = [run(W, True) for W in Ws]
+    for _ in range(3):
+        got = [run(W, False) for W in Ws]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+    assert st.item() == 0
+
+
+def test_empty_tensors(E):
+    st, none = _status(), _int([])
+    f, b, i8 = (torch.empty((0, 64), dtype=t, device="cuda") for t in (torch.float32, torch.bfloat16, torch.int8))
+    E.epara_rms_norm_i8(b, torch.ones(64, dtype=torch.bfloat16, device="cuda"), i8, f[:, 0], _st(), resid=f, resid_out=f)
+    p = _gemm_case(0, 64, 64, 0, 1)
+    E.epara_gemm_i8(dict(p, A=i8, a_scale=f[:, 0], C=b), _st(), st)
+    c = Cache(2, 64, 1, 64, 1)
+    before = c.codes.clone()
+    E.epara_kv8_append(b.view(0, 1, 64), b.view(0, 1, 64), c.codes, c.scales, none, c.tables[:0], 64, st, _st(), q_rows=_int([0]))
+    E.epara_kv8_append(b.view(0, 1, 64), b.view(0, 1, 64), c.codes, c.scales, _int([5, 9]), c.tables, 64, st, _st(), q_rows=_int([0, 0, 0]))
+    E.epara_kv8_attention(b, c.codes, c.scales, _int([5, 9]), c.tables, b, 1, 1, 64, 64, None, st, _st(), q_rows=_int([0, 0, 0]))
+    assert st.item() == 0 and torch.equal(before.view(torch.uint8), c.codes.view(torch.uint8))
+
+
+def test_calls_leave_the_current_device(E):
+    assert torch.cuda.current_device() == 0
+    x, q, s = torch.randn((2, 64), device="cuda"), torch.empty((2, 64), dtype=torch.int8, device="cuda"), torch.empty(2, device="cuda")
+    E.epara_rms_norm_i8(x, None, q, s, _st(), device=0)
+    with pytest.raises(E.EparaError) as e:                 # a device that is not there
+        E.epara_rms_norm_i8(x, None, q, s, _st(), device=63)
+    assert e.value.status == E.E_CUDA and torch.cuda.current_device() == 0
+    E.epara_rms_norm_i8(x, None, q, s, _st())
+    _check_norm(x, None, None, q, s, None)

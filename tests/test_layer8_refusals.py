@@ -31,6 +31,16 @@ def test_empty_calls_are_fine(E):
     assert _gemm(E, M=0) == E.OK
     assert _append(E, B=0, T=0) == E.OK and _append(E, T=0, q_rows=P) == E.OK
     assert _attn(E, B=0, T=0) == E.OK
+    # tensors without elements have no address
+    assert _norm(E, rows=0, x=None, q=None, scales=None) == E.OK and _gemm(E, M=0, A=None, C=None, a_scale=None) == E.OK
+    assert _append(E, B=0, T=0, k=None, v=None, lens=None, tables=None) == E.OK and _attn(E, B=0, T=0, q=None, out=None, lens=None, tables=None) == E.OK
+
+
+def test_norm_takes_no_other_type_for_bf16(E):
+    import torch
+    x = torch.zeros((1, 8), dtype=torch.float16)
+    with pytest.raises(TypeError):
+        E.epara_rms_norm_i8(x, None, torch.zeros((1, 8), dtype=torch.int8), torch.zeros(1), 0, device=0)
 
 
 def _gemm(E, status=P, **k):
@@ -47,8 +57,13 @@ def test_gemm_refuses(E, bad):
     assert _gemm(E, **bad) == E.E_INVALID
 
 
-def test_gemm_refuses_sums_past_31_bits(E):
-    assert _gemm(E, K=E.GEMM_I8_MAX_K + 1, lda=1 << 18, ldw=1 << 18) == E.E_UNSUPPORTED
+def test_sizes_beyond_what_is_counted_in_32_bits(E):
+    assert _gemm(E, K=E.GEMM_I8_MAX_K + 1, lda=1 << 18, ldw=1 << 18) == E.E_UNSUPPORTED          # sums past 31 bits
+    assert _gemm(E, M=(1 << 31) - 1, N=1 << 20, ldc=1 << 20) == E.E_UNSUPPORTED
+    big = (1 << 30) + 8
+    assert _norm(E, d=big, x_stride=big, resid_stride=big, resid_out_stride=big, q_stride=big) == E.E_UNSUPPORTED
+    for call in (_append, _attn):
+        assert call(E, max_len=big, table_stride=1 << 27) == E.E_UNSUPPORTED
 
 
 def _append(E, **k):
