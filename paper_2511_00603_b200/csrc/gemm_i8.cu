@@ -289,13 +289,13 @@ constexpr int PR_STAGE_OUT = PR_EPI_WARPS * 2048;   // epilogue staging: 32 rows
 constexpr size_t PR_SMEM = 1024 + (size_t)PR_RING + PR_STAGE_OUT + 256;
 constexpr int PR_ACC_COLS = 256;
 
-// Outputs of one warp for one tile: 32 rows (lane = row) x the part-th quarter of the tile's columns.  A chunk's values are parked in
+// Outputs of one warp for one tile: 32 rows (lane = row) x the part-th 64 of the tile's columns (32 of a tile 128 wide).  A chunk's values are parked in
 // the warp's staging area and leave it as 16-byte pieces of 64-byte row segments (MODE 2: additions at L2), or one by one where
 // rows of C do not start on 16 bytes or the matrix ends.  MODE: 0 bf16, 1 SwiGLU, 2 fp32 residual.
 template <int MODE>
 __device__ __forceinline__ void i8_epilogue(const I8Args& g, int m_base, int n0, uint32_t taddr, unsigned char* wst, int part, int lane, float as, uint32_t tempty) {
   constexpr int CW = MODE == 2 ? 16 : 32;           // accumulator columns of a chunk
-  const int cols = g.bn >> 2, c_begin = part * cols, c_end = min(c_begin + cols, g.N - n0);
+  const int cols = g.bn > 128 ? 64 : 32, c_begin = part * cols, c_end = min(min(c_begin + cols, g.bn), g.N - n0);
   if (c_begin >= c_end) {
     tc_fence_before();
     __syncwarp();
@@ -531,15 +531,16 @@ inline int swap_ring(int bn, long long ctas, int split, int sm_count) { return b
 // times of calls in a row with W cold, measured (estimate), swapped operands: 1 x 6144 x 4096 one range 9.5 (9.3), two 8.5 (8.6), four 8.6 (8.6);
 // 32 x 4096 x 14336 two ranges 15.4 (15.4), four 14.0 (14.5); 394 x 1000 x 776 tiles of 32 rows 5.3 (5.1), of 64 with two ranges 6.0 (6.3),
 // of 208 with two 11 (12.3); 128 x 4096 x 14336 with four 16.8 (16.4); 256 x 6144 x 4096 tiles of 96 rows 12.8 (13.9), pairs, 128 columns
-// 11.6 (11.6); 512 x 4096 x 4096 14.1 (16.0) and 12.3 (11.6); 96 x 28672 x 4096 31 (31), pairs, 256 columns 28 (27).
+// 11.6 (11.6); 512 x 4096 x 4096 14.1 (16.0) and 12.3 (11.6); 96 x 28672 x 4096 31 (31), pairs, 256 columns 28 (26), 224 27 (25); 512 x 6144 x 4096
+// on pairs, 128 / 192 / 256 columns 18.0 / 13.7 / 16.1 (18.8 / 13.6 / 15.5); 768 x 4096 x 14336 52 / 35 / 41 (54 / 36 / 43).
 I8Plan i8_plan(long long M, int N, int K, int sm_count) {
   const int kblocks = (K + KB - 1) / KB;
   const double w_mb = (double)N * K * 1e-6;
   I8Plan p = {I8_PAIR, 256, 1};
   double best = 1e30;
-  for (int bn = 128; bn <= 256; bn += 128) {
+  for (int bn = 128; bn <= 256; bn += 32) {
     const long long tiles = (M + 255) / 256 * ((N + bn - 1) / bn), pairs = sm_count / 2, rounds = (tiles + pairs - 1) / pairs;
-    const double t = 4.6 + std::max((double)rounds * kblocks * (bn == 256 ? 0.34 : 0.22), w_mb / 6.0) + 0.3 * (double)(rounds - 1);
+    const double t = 4.6 + std::max((double)rounds * kblocks * (0.1 + 0.00094 * bn), w_mb / 6.0) + 0.3 * (double)(rounds - 1);
     if (t < best) { best = t; p.bn = bn; }
   }
   if (M > 1024) return p;

@@ -166,6 +166,9 @@ SHAPES = [
     (0, 64, 64), (1, 1, 1), (1, 16, 16), (1, 4096, 4096), (3, 10, 511), (8, 1000, 776), (9, 257, 4099), (16, 2048, 8200), (16, 17, 33),
     (17, 128, 128), (17, 40, 16), (31, 1000, 777), (33, 4097, 513), (64, 512, 8192), (96, 6144, 4096), (128, 2048, 14336), (129, 130, 260), (200, 1000, 100),
     (257, 512, 1025), (394, 1000, 776), (512, 2048, 2048), (513, 1000, 777), (1000, 130, 4096), (1024, 4096, 128), (2000, 2050, 513), (4100, 260, 260),
+    (1030, 2050, 260), (600, 5000, 2000), (2100, 1500, 130),         # pairs, 160, 224 and 192 columns
+    (8200, 2048, 300), (3000, 5000, 140),                            # ... with several tiles each
+    (192, 2048, 14336), (250, 900, 4096), (100, 30000, 300),         # swapped operands: wide tiles in four ranges; two CTAs to an SM in several rounds
 ]
 
 
