@@ -589,13 +589,15 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   }
 }
 
-// Merge of the chunks of a row, one block per (row, query head): warps take chunks in turn.
+// Merge of the chunks of a row: W warps share a (row, query head) and take its chunks in turn.
 constexpr int MERGE_WARPS = 4;
-template <int HD>
+template <int HD, int W>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) kv8_merge_kernel(const Kv8Attn a) {
   constexpr int E = HD / 32;
   __shared__ float sm_m[MERGE_WARPS], sm_l[MERGE_WARPS], sm_o[MERGE_WARPS][HD];
-  const int i = blockIdx.x % a.max_q, b = blockIdx.x / a.max_q, h = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x / 32 % W, lane = threadIdx.x & 31;
+  const int i = blockIdx.x % a.max_q, b = blockIdx.x / a.max_q, h = blockIdx.y * (MERGE_WARPS / W) + threadIdx.x / (32 * W);
+  if (W == 1 && h >= a.Hkv * a.G) return;
   pdl_wait();
   int row0, n;
   new_rows(a.q_rows, b, a.T, row0, n);
@@ -608,12 +610,12 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) kv8_merge_kernel(const Kv8At
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
   constexpr int U = 4;                             // chunks in flight
-  for (int c0 = warp; c0 < chunks; c0 += MERGE_WARPS * U) {
+  for (int c0 = warp; c0 < chunks; c0 += W * U) {
     float2 ml[U];
     float2 v[U][E / 2];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int c = c0 + u * MERGE_WARPS;
+      const int c = c0 + u * W;
       ml[u] = make_float2(-INFINITY, 0.f);
       if (c < chunks) {
         const float* p = part + (size_t)c * (HD + 2);
@@ -634,12 +636,19 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) kv8_merge_kernel(const Kv8At
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (c0 + u * MERGE_WARPS < chunks) {
+      if (c0 + u * W < chunks) {
         const float f = ml[u].x == -INFINITY ? 1.f : exp2f(ml[u].x - m);    // (a chunk of NaN scores has no maximum)
         l += ml[u].y * f;
 #pragma unroll
         for (int e = 0; e < E / 2; ++e) { o[2 * e] += v[u][e].x * f; o[2 * e + 1] += v[u][e].y * f; }
       }
+  }
+  if constexpr (W == 1) {
+    const float inv = 1.f / l;
+    bf16* const out = a.out + qr * HD + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e] = f2bf(o[e] * inv);
+    return;
   }
   if (lane == 0) { sm_m[warp] = m; sm_l[warp] = l; }
 #pragma unroll
@@ -681,27 +690,31 @@ Chunks kv8_chunks(int B, long long items, int slots, int max_len) {
   return {whole64(items >= slots ? std::min(t, 2048ll) : t), 0};
 }
 
-// ... of the kernel for many rows: one CTA to an SM; a chunk of at least 512 tokens, so that what a CTA does around its loop stays small.
+// ... of the kernel for many rows, one CTA to an SM: as many as fill one round, for a chunk more is partial results to write and merge, and what a
+// CTA does around its loop, 9 us, once more.  One request, 512 new tokens after 7680, hd 128, 64 items: one chunk 151 us, two 99, four 121, five
+// 149; 1024 new tokens, 128 items: one 154, two 189; 256 after 3840, 32 items: one 83, four 46, five 70.
 int kv8_flash_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) {
   const long long items = B * tiles * Hkv, whole = ((long long)max_len + 63) / 64 * 64;
-  if (items >= sm_count) return (int)std::min<long long>(whole, 1 << 30);
-  const long long c = ((long long)max_len * items + 2 * sm_count - 1) / (2 * sm_count);
-  return (int)std::min(std::max((c + 63) / 64 * 64, 512ll), whole);
+  const long long n = std::max(sm_count / items, 1ll), c = (max_len + n - 1) / n;
+  return (int)std::min(std::min(std::max((c + 63) / 64 * 64, 512ll), whole), 1ll << 30);
 }
 
 struct AttnPlan { int nt, tiles, chunk, chunks, clustered; };      // nt 0: the kernel for many rows
-// Which kernel: beyond 16 query rows the one for many rows where the work, rows times the tokens of all kv heads, is large enough for its
-// tiles of 128 rows, most of them empty, to cost less than reading the cache again for every 16.  Device times, few rows and many, hd 128: 32
-// requests of 1024 to 2048 tokens, 20 rows 57 and 59 us, 32 rows 68 and 60; 8 of 2048 to 4096, 32 rows 32 and 46, 48 rows 50 and 49, 64 rows 62
-// and 52; one of 16384, 64 rows 37 and 41, 96 rows 46 and 45; one of 1000, 256 rows 19 and 32.  hd 64: 32 of 1024 to 2048, 48 rows 45 and 49, 64
-// rows 60 and 49; 8 of 2048 to 4096, 96 rows 44 and 45; one of 16384, 128 rows 37 and 37.
-// Tiles of 8 rows instead of 16 where contexts are short: 32 requests of up to 2048 tokens, 16 rows, hd 128 41 and 48 us; but 8 of up to 4096
-// 25 and 23.
+// Which kernel, by the rows of a (request, kv head): the one for many rows takes 256 at the price of one, mostly its exponentials, the other
+// one reads the cache again for every 16.  Device times, few rows and many, hd 128: 64 requests of 2048 to 4096 tokens, 32 rows 199 and 210 us,
+// 40 rows 275 and 212; 8 of them, 32 rows 33 and 42, 48 rows 50 and 44; one of 16384, 48 rows 32 and 29; one of 1000, 256 rows 20 and 32.  hd
+// 64: 64 of 2048 to 4096, 48 rows 156 and 176, 64 rows 202 and 176; one of 16384, 64 rows 23 and 24, 96 rows 28 and 25; one of 4096, 128 rows
+// 17 and 18.
+// Tiles of 8 rows or of 16: 64 requests of up to 512 tokens, 20 rows, hd 128 36 and 43 us, 32 rows 47 and 47; 64 of up to 4096, 20 rows 172 and
+// 190, 32 rows 224 and 199; 16 of up to 16384, 20 rows, hd 64 111 and 102; 32 of up to 2048, 16 rows 41 and 48; 8 of up to 4096, 16 rows 25
+// and 23.
 AttnPlan attn_plan(int B, int Hq, int Hkv, int hd, int max_q, int max_len, int sm_count) {
   AttnPlan p;
   const long long rows = (long long)max_q * (Hq / Hkv);
   const double work = (double)rows * B * Hkv * max_len;
-  p.nt = rows > 16 && work > (hd == 128 ? 12.5e6 : 22e6) ? 0 : rows <= 8 || (rows <= 32 && max_len <= 2048) ? 1 : 2;
+  const bool many = hd == 128 ? rows > 32 && work > 3e6 : rows > 48 && work > 9e6;
+  const bool eights = rows <= 8 || (rows <= 24 && max_len <= (rows <= 16 ? 2048 : 4096)) || (rows <= 32 && max_len <= 2048 && work <= 3e6);
+  p.nt = many ? 0 : eights ? 1 : 2;
   const int tile = p.nt ? 8 * p.nt : KV8_FLASH_ROWS;
   p.tiles = (int)((rows + tile - 1) / tile);
   p.clustered = 0;
@@ -716,10 +729,16 @@ AttnPlan attn_plan(int B, int Hq, int Hkv, int hd, int max_q, int max_len, int s
   return p;
 }
 
+// A warp to a (row, head), or four: 256 new tokens in 2 chunks, hd 128 63 and 70 us with the attention; 32 single tokens x 32 heads in 4 chunks of
+// few tokens 71 and 73; one token x 32 heads in 37 chunks 17 and 14.
+constexpr int KV8_MERGE_MANY = 2048;
 template <int HD>
 cudaError_t launch_merge(const Kv8Attn& a, cudaStream_t st) {
   if (a.max_chunks == 1) return cudaSuccess;
-  return launch_pdl(kv8_merge_kernel<HD>, dim3((unsigned)(a.B * a.max_q), (unsigned)(a.Hkv * a.G)), dim3(MERGE_WARPS * 32), 0, st, a);
+  const unsigned rows = (unsigned)(a.B * a.max_q), heads = (unsigned)(a.Hkv * a.G);
+  if ((long long)rows * heads >= KV8_MERGE_MANY)
+    return launch_pdl(kv8_merge_kernel<HD, 1>, dim3(rows, (heads + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, st, a);
+  return launch_pdl(kv8_merge_kernel<HD, MERGE_WARPS>, dim3(rows, heads), dim3(MERGE_WARPS * 32), 0, st, a);
 }
 
 template <int HD, int NT>

@@ -345,7 +345,7 @@ def test_attention_one_token(E, hd, Hkv, G):
     ([1, 2, 3, 0, 4], [1, 2, 3, 9, 500]), ([5, 16, 17, 1], [5, 16, 400, 77]), ([33, 0, 64, 100], [33, 1, 1000, 129]), ([130, 7, 257], [130, 900, 700]),
     ([600, 31], [1090, 600]), ([40, 4], [17, 2]),          # (fewer tokens than new rows: the first rows see none)
 ])
-@pytest.mark.parametrize("max_len", [1100, 4000, 1 << 20])     # the last one: the kernel for many rows wherever there are more than 16
+@pytest.mark.parametrize("max_len", [1100, 4000, 1 << 20])     # the last one: the kernel for many rows wherever there are more than 48
 def test_attention_several_tokens(E, hd, Hkv, G, ns, lens, max_len):
     c = Cache(len(ns), max_len, Hkv, hd, sum(ns) + G, used=1100)
     T = sum(ns)
@@ -363,6 +363,32 @@ def test_attention_long_context(E, hd):
         q = (2 * torch.randn((sum(ns), 8 * hd), generator=_gen(4), device="cuda")).to(torch.bfloat16)
         out, _ = _attend(E, c, q, lens, ns, 4)
         _check_attention(c, q, lens, ns, 4, out)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("Hkv,G", [(2, 4), (3, 3)])
+def test_attention_many_rows_in_several_chunks(E, hd, Hkv, G):
+    """Rows that end in each of the chunks, so many of them that a warp merges a row."""
+    c = Cache(2, 4000, Hkv, hd, 5)
+    for ns, lens in (([600, 500], [3900, 1500]), ([300, 1], [300, 4000])):
+        q = torch.randn((sum(ns), Hkv * G * hd), generator=_gen(6), device="cuda").to(torch.bfloat16)
+        out, st = _attend(E, c, q, lens, ns, G)
+        assert st.item() == 0
+        _check_attention(c, q, lens, ns, G, out)
+        again, _ = _attend(E, c, q, lens, ns, G)
+        assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_many_requests_in_several_chunks(E, hd):
+    B, Hkv, G = 300, 3, 3
+    c = Cache(B, 8192, Hkv, hd, 7, used=2200)
+    lens = [(37 * b) % 90 + 1 for b in range(B)]
+    lens[3], lens[150], lens[298], lens[299] = 2200, 2049, 2048, 0
+    q = torch.randn((B, Hkv * G * hd), generator=_gen(8), device="cuda").to(torch.bfloat16)
+    out, st = _attend(E, c, q, lens, [1] * B, G)
+    assert st.item() == 0
+    _check_attention(c, q, lens, [1] * B, G, out)
 
 
 @pytest.mark.parametrize("hd", [64, 128])
