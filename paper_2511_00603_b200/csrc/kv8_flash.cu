@@ -10,10 +10,18 @@
 //                   scores are read and reduced while the other keeps the special-function unit busy;
 //   warps 8, 9      issue S_g = Q_g K^T (M 128, N 64) into one of two buffers per tile, g = 0 and 1;
 //   warps 10, 11    issue O_g += P_g V, P as the A operand from tensor memory, V as an MN-major B operand;
-//   warps 12-15     request the pages of the next steps, one of each, and write them as the 128-byte-swizzled tiles that the MMAs want.  NaN codes of V are taken out (a zero probability times NaN is NaN) and the first key
-//                   that has one is kept per dim: a row that sees it gets its NaN at the end.
+//   warps 12-15     request the pages of the next steps, one of each, and write them as the 128-byte-swizzled tiles that the MMAs want.  NaN
+//                   codes of V are taken out (a zero probability times NaN is NaN) and the first key that has one is kept per dim: a row that
+//                   sees it gets its NaN at the end.
 // With several chunks of keys partial results go to scratch, as in the kernel for few rows, and are merged by the same kernel.
 // Every mbarrier wait is bounded.
+//
+// Bound by the tensor cores on paper (2 products of rows x keys x hd), in fact by no unit alone.  Four prompt chunks of 509 to 1024 new tokens
+// after up to 8192, 32 heads over 8, hd 128: 271 us, 877 TFLOP/s; hd 64: 216.  A step takes 2250 cycles: the tensor cores are at work in 1280
+// (an MMA of N 64 takes 3/4 of one of N 128, as all of Q is read for it), the special-function unit in 1024, shared memory, by its bytes, in
+// 1500.  Without any exponentials it would take 5 % less, without the conversion 4 %, with an eighth of Q K^T 4.5 %.  9 us of a CTA are not its
+// loop, and the last round of CTAs leaves 7 % of the SMs idle.  Tried: 16 softmax warps, two threads to a row, 295; 128 keys to a pass of the softmax, 295 (a longer chain from P V to
+// the next scores outweighs the fewer hand-overs); without turns 283; the page scales of a step fetched in the one before 267, but 219 for hd 64.
 #include <climits>
 
 #include "../../include/epara.h"
@@ -127,7 +135,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // ---- the work item.  The longest ones start first: requests in order of their lengths, of each one the last rows first.  (In order of
-  // the rows alone a long request with few rows came late: XXX us for the four prompt chunks, like this XXX.)
+  // the rows alone a long request with few rows came late: 362 us for the four prompt chunks, like this 283.)
   const int kvh = blockIdx.x % a.Hkv, nth = blockIdx.x / a.Hkv / a.tiles, pair = a.tiles - 1 - blockIdx.x / a.Hkv % a.tiles, chunk = blockIdx.y;
   __shared__ int the_request;
   pdl_wait();
@@ -214,7 +222,8 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     auto scale_of = [&](int id) { return id >= 0 ? a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh] : 0.f; };
     float vs_cur = scale_of(id_cur), vs_next = scale_of(id_next);
     // The pages of the next steps are requested as 16-byte asynchronous copies into a ring of this warp's own: a step is shorter than
-    // the way to memory (with one step's loads in registers 359 us for the four prompt chunks, like this XXX).
+    // the way to memory.  (By itself no faster than one step's loads in registers, 359 and 362 us for the four prompt chunks, but these
+    // registers are what the conversion needs.)
     const uint32_t raw = base + Geo::OFF_RAW + cw * Geo::RAW * Geo::RAW_BYTES;
     int where[NX], rawat[NX], place[NX];              // of a piece in the page tile, in the ring and in the converted tile (its first half)
 #pragma unroll
