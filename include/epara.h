@@ -447,6 +447,7 @@ int epara_kv8_append(int device, void* cuda_stream, const void* k, int k_stride,
  * [T, Hq*hd] at any 2-byte boundary.  kv_lens outside [0, max_len] are clamped.  A row that attends to no token, and rows that belong to no
  * request, are left unwritten.  A page id outside [0, kv_pages) is never dereferenced and leaves 102 in *status: the
  * request's outputs must not be used, the others are as they should be.
+ * Sizes whose rows of a kv head (max_q * Hq / Hkv), rows of all requests (B * max_q) or tiles pass 2^31, and more than 65535 heads, are UNSUPPORTED.
  * scratch: 16-byte aligned, epara_kv8_attention_scratch_bytes() with the same arguments (0: may be NULL); it holds partial results of the
  * call, nothing has to be cleared, calls that may overlap on the GPU need one each. */
 int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stride, const void* kv8_layer, const float* kv_scales, long long kv_pages,

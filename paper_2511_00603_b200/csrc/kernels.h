@@ -134,7 +134,8 @@ struct Kv8Append {
   const int32_t* tables;
   int* status;
   long long kv_pages;
-  int k_stride, v_stride, table_stride, T, Hkv, max_q, max_len, pages_per_request;
+  int k_stride, v_stride, table_stride, B, T, Hkv, max_q, max_len;
+  int pages_per_request;   // at most
 };
 struct Kv8Attn {
   const bf16* q;
@@ -144,14 +145,17 @@ struct Kv8Attn {
   const int32_t* kv_lens;
   const int32_t* tables;
   bf16* out;
-  float* partial;          // [T][Hq][max_chunks][hd + 2]: maximum, sum, unnormalised output
+  float* partial;          // [T, or B x part_tokens][Hq][max_chunks][hd + 2]: maximum, sum, unnormalised output
   int* status;
   long long kv_pages;
   int q_stride, table_stride, B, T, Hkv, G, max_q, max_len;
-  int tiles;               // row tiles of a request
+  int tiles;               // row tiles of a request with max_q new tokens
+  int min_n, max_n;        // new tokens of the requests that this launch takes
+  int part_tokens;         // 0: partial results by the rows of q, else so many for each request
   int chunk, max_chunks;   // tokens of a chunk, chunks of the longest request
 };
 constexpr int KV8_FLASH_ROWS = 256;      // query rows of a CTA in the kernel for many rows (kv8_flash.cu)
-cudaError_t launch_kv8_flash(const Kv8Attn& a, int hd, cudaStream_t st);
+constexpr int KV8_FLASH_SORTED = 1024;   // requests of a call that it puts in order
+cudaError_t launch_kv8_flash(const Kv8Attn& a, int hd, long long items, cudaStream_t st);       // items: row tiles of all requests, at least
 
 }  // namespace epara

@@ -20,16 +20,21 @@ constexpr int PAGE = EPARA_KV_PAGE;
 // ------------------------------------------------------------------------------------------------ append
 // A block takes one page of one request, a warp one (K or V, kv head) of it: 16 x hd values in registers, so the maximum, the
 // scale and the codes come out of one read.  Bound by HBM: 24 chunks of 65 to 1024 tokens, 8 kv heads, hd 128 14.5 us, floor 12.3 (bf16 in, a byte and
-// 1/512 of a scale an element out); one token of each of 64 requests 2.7 us, a launch.
+// 1/512 of a scale an element out); one token of each of 64 requests 2.6 us, a launch.
+// Blocks: for each request as many as max_q tokens can lie on pages; BY_ROW, where few requests have that many, one for each row of k, which
+// takes the page that its row is the first one on (256 requests with one token beside 1024 of another: 39 and 9 us).
 constexpr int APPEND_WARPS = 8;
 
-template <int HD>
+template <int HD, bool BY_ROW>
 __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8Append a) {
   constexpr int LPR = HD / 8, TPL = 32 / LPR, NL = PAGE / TPL;    // lanes to a token (8 values each), tokens to a load, loads
   pdl_wait();
-  const int b = blockIdx.x / a.pages_per_request, j = blockIdx.x % a.pages_per_request;
+  const int b = BY_ROW ? request_of(a.q_rows, a.B, blockIdx.x) : blockIdx.x / a.pages_per_request;
+  if (BY_ROW && b >= a.B) return;
   int row, n;
   new_rows(a.q_rows, b, a.T, row, n);
+  const int j = BY_ROW ? (int)blockIdx.x - row : blockIdx.x % a.pages_per_request;     // page of the new tokens, or token
+  if (BY_ROW && (j < 0 || j >= min(n, a.max_q))) return;
   const int len = a.kv_lens[b];
   if (threadIdx.x == 0 && blockIdx.y == 0 && j == 0) {
     if (n > a.max_q) atomicExch(a.status, ERR_ROWS);
@@ -38,7 +43,8 @@ __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8
   if (n <= 0 || len < n || len > a.max_len) return;
   const int first = len - n;                       // position of the first new token
   const int end = first + min(n, a.max_q);
-  const int pg = first / PAGE + j;
+  if (BY_ROW && j > 0 && (first + j) % PAGE != 0) return;           // the page is another row's
+  const int pg = BY_ROW ? (first + j) / PAGE : first / PAGE + j;
   if (pg * PAGE >= end) return;
   const int lane = threadIdx.x & 31, t0 = lane / LPR, c = lane % LPR;
   const int s0 = max(first - pg * PAGE, 0), s1 = min(end - pg * PAGE, PAGE);   // the page's new slots
@@ -203,7 +209,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
     n = a.max_q;
   }
   const int rows = min(n * G - tile * TR, TR);     // of this tile
-  if (rows <= 0) return;
+  if (rows <= 0 || n > a.max_n) return;
   const int seen_top = seen0 + (tile * TR + rows - 1) / G;
   const int t_begin = chunk * a.chunk, t_end = min(seen_top, t_begin + a.chunk);
   if (!CLUSTER && t_begin >= t_end) return;        // (a block of a cluster goes on with no pages)
@@ -555,7 +561,8 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
     } else if (sees <= a.chunk) {
       store(q_row(r), d, ox / ll, oy / ll);
     } else {
-      float* const part = a.partial + (q_row(r) * a.max_chunks + chunk) * (HD + 2);
+      const size_t at = a.part_tokens ? ((size_t)b * a.part_tokens + (tile * TR + r) / G) * a.Hkv * G + kvh * G + (tile * TR + r) % G : q_row(r);
+      float* const part = a.partial + (at * a.max_chunks + chunk) * (HD + 2);
       __stcg(reinterpret_cast<float2*>(part + 2 + d), make_float2(ox, oy));
       if (d == 0) __stcg(reinterpret_cast<float2*>(part), make_float2(mm, ll));
     }
@@ -593,23 +600,30 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   }
 }
 
-// Merge of the chunks of a row: W warps share a (row, query head) and take its chunks in turn.
+// Merge of the chunks of a row: W warps share a (row, query head) and take its chunks in turn.  BY_ROW: a block to a row of q instead of one to
+// each of the most rows that a request may have: most of them would have none where one request of many has a long prompt chunk.
 constexpr int MERGE_WARPS = 4;
-template <int HD, int W>
-__global__ void __launch_bounds__(MERGE_WARPS * 32) kv8_merge_kernel(const Kv8Attn a) {
+template <int HD, int W, bool BY_ROW>
+__global__ void __launch_bounds__(MERGE_WARPS * 32) kv8_merge_kernel(const Kv8Attn a, int tokens) {
   constexpr int E = HD / 32;
   __shared__ float sm_m[MERGE_WARPS], sm_l[MERGE_WARPS], sm_o[MERGE_WARPS][HD];
   const int warp = threadIdx.x / 32 % W, lane = threadIdx.x & 31;
-  const int i = blockIdx.x % a.max_q, b = blockIdx.x / a.max_q, h = blockIdx.y * (MERGE_WARPS / W) + threadIdx.x / (32 * W);
+  const int h = blockIdx.y * (MERGE_WARPS / W) + threadIdx.x / (32 * W);
   if (W == 1 && h >= a.Hkv * a.G) return;
   pdl_wait();
+  const int b = BY_ROW ? request_of(a.q_rows, a.B, blockIdx.x) : blockIdx.x / tokens;
+  if (b >= a.B) return;
   int row0, n;
   new_rows(a.q_rows, b, a.T, row0, n);
-  const int sees = min(max(a.kv_lens[b], 0), a.max_len) - n + i + 1;
+  const int i = BY_ROW ? (int)blockIdx.x - row0 : blockIdx.x % tokens, all = n;
+  n = min(n, a.max_q);
+  if (i < 0 || n < a.min_n || n > a.max_n) return;
+  const int sees = min(max(a.kv_lens[b], 0), a.max_len) - all + i + 1;
   if (i >= n || sees <= a.chunk) return;
   const int chunks = (sees + a.chunk - 1) / a.chunk;
   const size_t qr = (size_t)(row0 + i) * a.Hkv * a.G + h;
-  const float* const part = a.partial + qr * a.max_chunks * (HD + 2);
+  const size_t at = a.part_tokens ? ((size_t)b * a.part_tokens + i) * a.Hkv * a.G + h : qr;
+  const float* const part = a.partial + at * a.max_chunks * (HD + 2);
   float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
@@ -697,13 +711,20 @@ Chunks kv8_chunks(int B, long long items, int slots, int max_len) {
 // ... of the kernel for many rows, one CTA to an SM: as many as fill one round, for a chunk more is partial results to write and merge, and what a
 // CTA does around its loop, 9 us, once more.  One request, 512 new tokens after 7680, hd 128, 64 items: one chunk 151 us, two 99, four 121, five
 // 149; 1024 new tokens, 128 items: one 154, two 189; 256 after 3840, 32 items: one 83, four 46, five 70.
-int kv8_flash_chunk(long long B, int tiles, int Hkv, int max_len, int sm_count) {
-  const long long items = B * tiles * Hkv, whole = ((long long)max_len + 63) / 64 * 64;
+int kv8_flash_chunk(long long requests, int tiles, int Hkv, int max_len, int sm_count) {
+  const long long items = requests * tiles * Hkv, whole = ((long long)max_len + 63) / 64 * 64;
   const long long n = std::max(sm_count / items, 1ll), c = (max_len + n - 1) / n;
   return (int)std::min(std::min(std::max((c + 63) / 64 * 64, 512ll), whole), 1ll << 30);
 }
 
-struct AttnPlan { int nt, tiles, chunk, chunks, clustered; };      // nt 0: the kernel for many rows
+// A call whose requests differ is split where the longest ones are for the kernel for many rows: those of up to few_tokens new tokens go to the
+// other one, in a launch of its own.  (256 requests of 1000 to 2000 tokens with one token each beside 1024 of a prompt, hd 128: 1595 us when all go to
+// the kernel for many rows; 184 like this, 135 and 31 apart.)
+struct AttnPlan {
+  int nt, tiles, chunk, chunks, clustered;           // nt 0: the kernel for many rows
+  int few_tokens, few_nt, few_tiles, few_chunk, few_chunks, few_clustered;         // few_tokens 0: not split
+  long long many_items;                              // row tiles of the kernel for many rows
+};
 // Which kernel, by the rows of a (request, kv head): the one for many rows takes 256 at the price of one, mostly its exponentials, the other
 // one reads the cache again for every 16.  Device times, few rows and many, hd 128: 64 requests of 2048 to 4096 tokens, 32 rows 199 and 210 us,
 // 40 rows 275 and 212; 8 of them, 32 rows 33 and 42, 48 rows 50 and 44; one of 16384, 48 rows 32 and 29; one of 1000, 256 rows 20 and 32.  hd
@@ -712,37 +733,67 @@ struct AttnPlan { int nt, tiles, chunk, chunks, clustered; };      // nt 0: the 
 // Tiles of 8 rows or of 16: 64 requests of up to 512 tokens, 20 rows, hd 128 36 and 43 us, 32 rows 47 and 47; 64 of up to 4096, 20 rows 172 and
 // 190, 32 rows 224 and 199; 16 of up to 16384, 20 rows, hd 64 111 and 102; 32 of up to 2048, 16 rows 41 and 48; 8 of up to 4096, 16 rows 25
 // and 23.
-AttnPlan attn_plan(int B, int Hq, int Hkv, int hd, int max_q, int max_len, int sm_count) {
-  AttnPlan p;
-  const long long rows = (long long)max_q * (Hq / Hkv);
+AttnPlan attn_plan(int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len, int sm_count) {
+  AttnPlan p = {};
+  const int G = Hq / Hkv;
+  const long long rows = (long long)max_q * G;
   const double work = (double)rows * B * Hkv * max_len;
   const bool many = hd == 128 ? rows > 32 && work > 3e6 : rows > 48 && work > 9e6;
   const bool eights = rows <= 8 || (rows <= 24 && max_len <= (rows <= 16 ? 2048 : 4096)) || (rows <= 32 && max_len <= 2048 && work <= 3e6);
   p.nt = many ? 0 : eights ? 1 : 2;
   const int tile = p.nt ? 8 * p.nt : KV8_FLASH_ROWS;
   p.tiles = (int)((rows + tile - 1) / tile);
-  p.clustered = 0;
+  auto few = [&](int nt, long long tiles) { return kv8_chunks(B, (long long)B * tiles * Hkv, (nt == 1 ? 4 : 3) * sm_count, max_len); };
   if (p.nt) {
-    const Chunks c = kv8_chunks(B, (long long)B * p.tiles * Hkv, (p.nt == 1 ? 4 : 3) * sm_count, max_len);
+    const Chunks c = few(p.nt, p.tiles);
     p.chunk = c.tokens;
     p.clustered = c.clustered;
   } else {
-    p.chunk = kv8_flash_chunk(B, p.tiles, Hkv, max_len, sm_count);
+    p.chunk = kv8_flash_chunk(std::min(std::max(T / max_q, 1), B), p.tiles, Hkv, max_len, sm_count);
+    const int few_rows = G <= 16 ? 16 : 32;
+    if (G <= few_rows && T <= (long long)(B - 1) * max_q + few_rows / G) {             // (else none can be as short)
+      p.few_tokens = few_rows / G;
+      p.few_nt = G <= 8 ? 1 : 2;
+      p.few_tiles = (p.few_tokens * G + 8 * p.few_nt - 1) / (8 * p.few_nt);
+      const Chunks c = few(p.few_nt, (G + 8 * p.few_nt - 1) / (8 * p.few_nt));
+      p.few_chunk = c.tokens;
+      p.few_clustered = c.clustered;
+      p.few_chunks = (max_len + p.few_chunk - 1) / p.few_chunk;
+    }
+    // every request adds at most one tile to those that the rows fill
+    p.many_items = (long long)B * p.tiles;
+    if (B <= KV8_FLASH_SORTED) p.many_items = std::min(p.many_items, (long long)T * G / KV8_FLASH_ROWS + std::min(B, T / (p.few_tokens + 1)));
   }
   p.chunks = (max_len + p.chunk - 1) / p.chunk;
   return p;
+}
+// ... and what it counts fits 32 bits
+bool attn_countable(long long B, int Hq, int Hkv, long long max_q) {
+  const long long rows = max_q * (Hq / Hkv), tiles = rows / 8 + 1;
+  return Hq <= 65535 && rows < (1ll << 31) - 1024 && B * max_q < 1ll << 31 && B * tiles * Hkv < 1ll << 31;
+}
+size_t many_scratch(const AttnPlan& p, int T, int Hq, int hd) { return p.chunks == 1 || p.clustered ? 0 : (size_t)T * Hq * p.chunks * (hd + 2) * sizeof(float); }
+size_t few_scratch(const AttnPlan& p, int B, int Hq, int hd) {
+  return p.few_tokens == 0 || p.few_chunks == 1 || p.few_clustered ? 0 : (size_t)B * p.few_tokens * Hq * p.few_chunks * (hd + 2) * sizeof(float);
 }
 
 // A warp to a (row, head), or four: 256 new tokens in 2 chunks, hd 128 63 and 70 us with the attention; 32 single tokens x 32 heads in 4 chunks of
 // few tokens 71 and 73; one token x 32 heads in 37 chunks 17 and 14.
 constexpr int KV8_MERGE_MANY = 2048;
+template <int HD, int W, bool BY_ROW>
+cudaError_t launch_merge_as(const Kv8Attn& a, unsigned rows, int tokens, cudaStream_t st) {
+  const unsigned heads = (unsigned)(a.Hkv * a.G), per = MERGE_WARPS / W;
+  return launch_pdl(kv8_merge_kernel<HD, W, BY_ROW>, dim3(rows, (heads + per - 1) / per), dim3(MERGE_WARPS * 32), 0, st, a, tokens);
+}
 template <int HD>
 cudaError_t launch_merge(const Kv8Attn& a, cudaStream_t st) {
   if (a.max_chunks == 1) return cudaSuccess;
-  const unsigned rows = (unsigned)(a.B * a.max_q), heads = (unsigned)(a.Hkv * a.G);
-  if ((long long)rows * heads >= KV8_MERGE_MANY)
-    return launch_pdl(kv8_merge_kernel<HD, 1>, dim3(rows, (heads + MERGE_WARPS - 1) / MERGE_WARPS), dim3(MERGE_WARPS * 32), 0, st, a);
-  return launch_pdl(kv8_merge_kernel<HD, MERGE_WARPS>, dim3(rows, heads), dim3(MERGE_WARPS * 32), 0, st, a);
+  const int tokens = std::min(a.max_q, a.max_n);
+  const bool by_row = a.q_rows && a.T < (long long)a.B * tokens;
+  const unsigned rows = (unsigned)(by_row ? a.T : a.B * tokens);
+  const bool warp_each = (long long)rows * a.Hkv * a.G >= KV8_MERGE_MANY;
+  if (by_row) return warp_each ? launch_merge_as<HD, 1, true>(a, rows, tokens, st) : launch_merge_as<HD, MERGE_WARPS, true>(a, rows, tokens, st);
+  return warp_each ? launch_merge_as<HD, 1, false>(a, rows, tokens, st) : launch_merge_as<HD, MERGE_WARPS, false>(a, rows, tokens, st);
 }
 
 template <int HD, int NT>
@@ -772,12 +823,26 @@ cudaError_t launch_few(const Kv8Attn& a, bool clustered, cudaStream_t st) {
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
+template <int HD>
+cudaError_t launch_few(const Kv8Attn& a, int nt, bool clustered, cudaStream_t st) {
+  return nt == 1 ? launch_few<HD, 1>(a, clustered, st) : launch_few<HD, 2>(a, clustered, st);
+}
 
 template <int HD>
-cudaError_t launch_attn(const Kv8Attn& a, const AttnPlan& p, cudaStream_t st) {
-  if (p.nt == 1) return launch_few<HD, 1>(a, p.clustered, st);
-  if (p.nt == 2) return launch_few<HD, 2>(a, p.clustered, st);
-  const cudaError_t e = launch_kv8_flash(a, HD, st);
+cudaError_t launch_attn(Kv8Attn a, const AttnPlan& p, cudaStream_t st) {
+  a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
+  a.min_n = 1; a.max_n = a.max_q; a.part_tokens = 0;
+  if (p.nt) return launch_few<HD>(a, p.nt, p.clustered, st);
+  if (p.few_tokens) {
+    Kv8Attn f = a;
+    f.tiles = p.few_tiles; f.chunk = p.few_chunk; f.max_chunks = p.few_chunks;
+    f.max_n = f.part_tokens = p.few_tokens;
+    f.partial = reinterpret_cast<float*>(reinterpret_cast<char*>(a.partial) + many_scratch(p, a.T, a.Hkv * a.G, HD));
+    const cudaError_t e = launch_few<HD>(f, p.few_nt, p.few_clustered, st);
+    if (e != cudaSuccess) return e;
+    a.min_n = p.few_tokens + 1;
+  }
+  const cudaError_t e = launch_kv8_flash(a, HD, p.many_items, st);
   return e == cudaSuccess ? launch_merge<HD>(a, st) : e;
 }
 
@@ -814,21 +879,27 @@ int epara_kv8_append(int device, void* cuda_stream, const void* k, int k_stride,
   a.q_rows = q_rows; a.kv_lens = kv_lens; a.tables = tables; a.status = status; a.kv_pages = kv_pages;
   a.k_stride = k_stride; a.v_stride = v_stride; a.table_stride = table_stride; a.T = T; a.Hkv = Hkv; a.max_len = max_len;
   a.max_q = std::min(max_q, T);
+  a.B = B;
   a.pages_per_request = (std::min(a.max_q, max_len) + PAGE - 2) / PAGE + 1;
-  if ((long long)B * a.pages_per_request > 0x7fffffffll) return EPARA_E_UNSUPPORTED;
+  const long long blocks = (long long)B * a.pages_per_request;
+  const bool by_row = q_rows && blocks > 2ll * T;
+  if (!by_row && blocks > 0x7fffffffll) return EPARA_E_UNSUPPORTED;
   const DeviceScope scope(device);
   if (!scope.ok) return EPARA_E_CUDA;
-  const dim3 grid((unsigned)(B * a.pages_per_request), (unsigned)((2 * Hkv + APPEND_WARPS - 1) / APPEND_WARPS));
-  const cudaError_t e = hd == 128 ? launch_pdl(kv8_append_kernel<128>, grid, dim3(APPEND_WARPS * 32), 0, (cudaStream_t)cuda_stream, a)
-                                  : launch_pdl(kv8_append_kernel<64>, grid, dim3(APPEND_WARPS * 32), 0, (cudaStream_t)cuda_stream, a);
+  const dim3 grid((unsigned)(by_row ? T : blocks), (unsigned)((2 * Hkv + APPEND_WARPS - 1) / APPEND_WARPS));
+  const auto kernel = hd == 128 ? (by_row ? kv8_append_kernel<128, true> : kv8_append_kernel<128, false>)
+                                : (by_row ? kv8_append_kernel<64, true> : kv8_append_kernel<64, false>);
+  const cudaError_t e = launch_pdl(kernel, grid, dim3(APPEND_WARPS * 32), 0, (cudaStream_t)cuda_stream, a);
   return e == cudaSuccess ? EPARA_OK : EPARA_E_CUDA;
 }
 
 size_t epara_kv8_attention_scratch_bytes(int device, int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len) {
   using namespace epara;
   if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || hd <= 0 || max_q <= 0 || max_len <= 0) return 0;
-  const AttnPlan p = attn_plan(B, Hq, Hkv, hd, std::min(max_q, T), max_len, device_sm_count(device));
-  return p.chunks == 1 || p.clustered ? 0 : (size_t)T * Hq * p.chunks * (hd + 2) * sizeof(float);
+  max_q = std::min(max_q, T);
+  if (!attn_countable(B, Hq, Hkv, max_q)) return 0;
+  const AttnPlan p = attn_plan(B, T, Hq, Hkv, hd, max_q, max_len, device_sm_count(device));
+  return many_scratch(p, T, Hq, hd) + few_scratch(p, B, Hq, hd);
 }
 
 int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stride, const void* kv8_layer, const float* kv_scales, long long kv_pages,
@@ -841,7 +912,7 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
   const int c = check_cache(kv8_layer, kv_scales, kv_pages, q_rows, kv_lens, tables, table_stride, B, T, Hkv, hd, max_q, max_len, status);
   if (c != EPARA_OK) return c;
   if ((long long)q_stride < (long long)Hq * hd) return EPARA_E_INVALID;
-  if (Hq > 65535) return EPARA_E_UNSUPPORTED;
+  if (!attn_countable(B, Hq, Hkv, std::min(max_q, T))) return EPARA_E_UNSUPPORTED;
   const size_t need = epara_kv8_attention_scratch_bytes(device, B, T, Hq, Hkv, hd, max_q, max_len);
   if (scratch_bytes < need) return EPARA_E_RESOURCE;
   if (need && (!scratch || !aligned(scratch, 16))) return EPARA_E_INVALID;
@@ -849,9 +920,8 @@ int epara_kv8_attention(int device, void* cuda_stream, const void* q, int q_stri
   a.q = (const bf16*)q; a.codes = (const unsigned char*)kv8_layer; a.scales = kv_scales; a.q_rows = q_rows; a.kv_lens = kv_lens; a.tables = tables;
   a.out = (bf16*)out; a.partial = (float*)scratch; a.status = status; a.kv_pages = kv_pages;
   a.q_stride = q_stride; a.table_stride = table_stride; a.B = B; a.T = T; a.Hkv = Hkv; a.G = Hq / Hkv; a.max_q = std::min(max_q, T); a.max_len = max_len;
-  const AttnPlan p = attn_plan(B, Hq, Hkv, hd, a.max_q, max_len, device_sm_count(device));
-  a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
-  if ((long long)B * a.tiles * Hkv > 0x7fffffffll || (long long)B * a.max_q > 0x7fffffffll || a.max_chunks > 65535) return EPARA_E_UNSUPPORTED;
+  const AttnPlan p = attn_plan(B, T, Hq, Hkv, hd, a.max_q, max_len, device_sm_count(device));
+  if (p.chunks > 65535 || p.few_chunks > 65535) return EPARA_E_UNSUPPORTED;
   const DeviceScope scope(device);
   if (!scope.ok) return EPARA_E_CUDA;
   const cudaError_t e = hd == 128 ? launch_attn<128>(a, p, (cudaStream_t)cuda_stream) : launch_attn<64>(a, p, (cudaStream_t)cuda_stream);

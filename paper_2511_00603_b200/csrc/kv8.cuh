@@ -32,6 +32,17 @@ __device__ __forceinline__ void new_rows(const int32_t* q_rows, int b, int T, in
   n = min(max(q_rows[b + 1], row), T) - row;
 }
 
+// The request of row t, by a converged warp: how many requests end at or before it (B: none has it).  32 looks at a time.
+__device__ __forceinline__ int request_of(const int32_t* q_rows, int B, int t) {
+  int lo = 0, hi = B;
+  while (lo < hi) {
+    const int step = (hi - lo + 31) / 32, c = __popc(__ballot_sync(0xffffffffu, q_rows[min(lo + ((int)(threadIdx.x & 31) + 1) * step, hi)] <= t));
+    hi = c == 32 ? hi : min(lo + (c + 1) * step, hi) - 1;
+    lo = c == 32 ? hi : lo + c * step;
+  }
+  return lo;
+}
+
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }

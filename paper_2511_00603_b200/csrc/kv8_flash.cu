@@ -41,7 +41,6 @@ constexpr int KF_S_WARP = 8, KF_PV_WARP = 10, KF_CONV_WARP = 12, KF_CONV_WARPS =
 constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
 constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
 constexpr float KF_RAISE = 8.0f;
-constexpr int KF_SORTED = 512;                        // requests of a call that are put in order
 
 template <int HD>
 struct KfGeo {
@@ -136,22 +135,38 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
 
   // ---- the work item.  The longest ones start first: requests in order of their lengths, of each one the last rows first.  (In order of
   // the rows alone a long request with few rows came late: 362 us for the four prompt chunks, like this 283.)
-  const int kvh = blockIdx.x % a.Hkv, nth = blockIdx.x / a.Hkv / a.tiles, pair = a.tiles - 1 - blockIdx.x / a.Hkv % a.tiles, chunk = blockIdx.y;
-  __shared__ int the_request;
+  const int kvh = blockIdx.x % a.Hkv, item = blockIdx.x / a.Hkv, chunk = blockIdx.y;
+  __shared__ int the_request, the_tile, all_tiles, all_live;
   pdl_wait();
-  int b = nth;
-  if (a.B > 1 && a.B <= KF_SORTED) {
+  int b = item / a.tiles, pair = a.tiles - 1 - item % a.tiles;
+  if (a.B <= KV8_FLASH_SORTED) {
+    int4* const live = reinterpret_cast<int4*>(base_ptr);             // length, request, tiles of those that this launch takes
+    if (threadIdx.x == 0) { all_tiles = all_live = 0; the_request = -1; }
+    __syncthreads();
     for (int i = threadIdx.x; i < a.B; i += KF_THREADS) {
-      const int mine = a.kv_lens[i];
+      int row0, n;
+      new_rows(a.q_rows, i, a.T, row0, n);
+      n = min(n, a.max_q);
+      if (n < a.min_n) continue;
+      const int tiles = (n * a.G + 2 * KF_TILE - 1) / (2 * KF_TILE);
+      live[atomicAdd(&all_live, 1)] = make_int4(a.kv_lens[i], i, tiles, 0);          // (in any order: what follows looks at lengths and requests)
+      atomicAdd(&all_tiles, tiles);
+    }
+    __syncthreads();
+    if (item >= all_tiles) return;
+    for (int i = threadIdx.x; i < all_live; i += KF_THREADS) {
+      const int4 own = live[i];
       int before = 0;
-      for (int k = 0; k < a.B; ++k) {
-        const int other = a.kv_lens[k];
-        before += other > mine || (other == mine && k < i);
+      for (int k = 0; k < all_live; ++k) {
+        const int4 other = live[k];
+        if (other.x > own.x || (other.x == own.x && other.y < own.y)) before += other.z;
       }
-      if (before == nth) the_request = i;
+      if (item >= before && item < before + own.z) { the_request = own.y; the_tile = own.z - 1 - (item - before); }
     }
     __syncthreads();
     b = the_request;
+    pair = the_tile;
+    if (b < 0) return;                                // (prefix sums that are none)
   }
   int row0, n;
   new_rows(a.q_rows, b, a.T, row0, n);
@@ -161,6 +176,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     if (threadIdx.x == 0 && pair == 0 && kvh == 0 && chunk == 0) atomicExch(a.status, ERR_ROWS);
     n = a.max_q;
   }
+  if (n < a.min_n) return;
   const int r_first = pair * 2 * KF_TILE, rows = min(n * G - r_first, 2 * KF_TILE);
   if (rows <= 0) return;
   const int t_begin = chunk * a.chunk, t_end = min(seen0 + (r_first + rows - 1) / G, t_begin + a.chunk);
@@ -554,14 +570,14 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
 }
 
 template <int HD>
-cudaError_t launch_as(const Kv8Attn& a, cudaStream_t st) {
+cudaError_t launch_as(const Kv8Attn& a, long long items, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(kv8_flash_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, KfGeo<HD>::SMEM);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kv8_flash_kernel<HD>, dim3((unsigned)(a.B * a.Hkv * a.tiles), (unsigned)a.max_chunks), dim3(KF_THREADS), KfGeo<HD>::SMEM, st, a);
+  return launch_pdl(kv8_flash_kernel<HD>, dim3((unsigned)(items * a.Hkv), (unsigned)a.max_chunks), dim3(KF_THREADS), KfGeo<HD>::SMEM, st, a);
 }
 
 }  // namespace
 
-cudaError_t launch_kv8_flash(const Kv8Attn& a, int hd, cudaStream_t st) { return hd == 128 ? launch_as<128>(a, st) : launch_as<64>(a, st); }
+cudaError_t launch_kv8_flash(const Kv8Attn& a, int hd, long long items, cudaStream_t st) { return hd == 128 ? launch_as<128>(a, items, st) : launch_as<64>(a, items, st); }
 
 }  // namespace epara

@@ -379,6 +379,50 @@ def test_attention_many_rows_in_several_chunks(E, hd, Hkv, G):
         assert torch.equal(out, again)
 
 
+MIXED = [([1] * 9 + [300] + [1] * 7, 16), ([700, 0, 1, 2, 3, 4, 5, 6, 16, 17, 33, 0], 5), ([0, 64, 1, 0, 130], 2), ([90] + [1, 0] * 260, 3), ([1] * 30 + [50, 60], 31)]
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("Hkv,G", [(2, 4), (1, 1), (3, 3), (1, 8), (2, 16), (1, 17), (1, 33)])
+@pytest.mark.parametrize("ns,seed", MIXED)
+@pytest.mark.parametrize("max_len", [3000, 40000])
+def test_attention_of_short_and_long_requests_in_one_call(E, hd, Hkv, G, ns, seed, max_len):
+    """Single tokens beside prompt chunks: each goes to its kernel, with chunks of its own; requests without rows and rows without requests."""
+    c = Cache(len(ns), max_len, Hkv, hd, seed, used=2500 if len(ns) < 40 else 700)
+    lens = [n + (181 * i + 7 * seed) % (2500 - 700 if len(ns) < 40 else 600) if n else 5 * i % 40 for i, n in enumerate(ns)]
+    T = sum(ns)
+    q = torch.randn((T + 5, Hkv * G * hd), generator=_gen(seed), device="cuda").to(torch.bfloat16)
+    out, st = _attend(E, c, q, lens, ns, G)
+    assert st.item() == 0
+    if len(ns) > 40:
+        pick = [0, 1, 2, 3, 101, 399, 519, 520]
+        _, starts = _rows(ns)
+        for b in pick:
+            _check_attention(Part(c, b), q, [lens[b]], [ns[b]], G, out, f"request {b}", row0=starts[b])
+    else:
+        _check_attention(c, q, lens, ns, G, out)
+    assert (out[T:] == 55).all()
+    again, _ = _attend(E, c, q, lens, ns, G)
+    assert torch.equal(out, again)
+    # rows before the first request, and what max_q cuts off
+    rows = _int([3 + r for r in _rows(ns)[1]])
+    moved, st = _attend(E, c, torch.cat([q[:3], q[:T]]), lens, ns, G, q_rows=rows)
+    assert st.item() == 0 and (moved[:3] == 55).all()
+    if len(ns) < 40:
+        _check_attention(c, torch.cat([q[:3], q[:T]]), lens, ns, G, moved, "moved", row0=3)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_long_requests_cut_off_beside_short_ones(E, hd):
+    ns, lens = [1, 80, 2, 50], [700, 900, 30, 1000]
+    c = Cache(4, 3000, 2, hd, 3, used=1000)
+    q = torch.randn((133, 8 * hd), generator=_gen(3), device="cuda").to(torch.bfloat16)
+    out, st = _attend(E, c, q, lens, ns, 4, max_q=60)
+    assert st.item() == E.ERR_ROWS and (out[61:81] == 55).all()
+    for b, row, n, L in ((0, 0, 1, 700), (1, 1, 60, 880), (2, 81, 2, 30), (3, 83, 50, 1000)):
+        _check_attention(Part(c, b), q, [L], [n], 4, out, row0=row)
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 def test_attention_many_requests_in_several_chunks(E, hd):
     B, Hkv, G = 300, 3, 3
@@ -532,6 +576,32 @@ def test_append(E, hd, Hkv, ns, lens):
     assert st.item() == 0 and torch.equal(c.scales.to(F64), want[1].to(torch.float32).to(F64))
     if lens[0] - ns[0] == 0:                               # (with the foreign scale still in use a quotient is not exact)
         assert _same(c.codes.to(F64), want[0])
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_append_single_tokens_beside_a_prompt(E, hd):
+    """Few of the requests have as many tokens as the longest: the same cache as by a call for each."""
+    ns = [1] * 30 + [0, 257, 0, 16, 1, 17] + [1] * 30
+    lens = [n + (7 * i) % 50 if n else 9 for i, n in enumerate(ns)]
+    g = _gen(4)
+    x = torch.randn((sum(ns) + 4, 6, hd), generator=g, device="cuda").to(torch.bfloat16)
+    one, each = Cache(len(ns), 400, 3, hd, 4), Cache(len(ns), 400, 3, hd, 4)
+    st = _status()
+    rows = [r + 2 for r in _rows(ns)[1]]                       # (two rows of nobody at both ends)
+    E.epara_kv8_append(x[:, :3], x[:, 3:], one.codes, one.scales, _int(lens), one.tables, 400, st, _st(), q_rows=_int(rows), max_q=257)
+    assert st.item() == 0
+    for b, n in enumerate(ns):
+        if n:
+            y = x[rows[b]:rows[b] + n]
+            E.epara_kv8_append(y[:, :3], y[:, 3:], each.codes, each.scales, _int([lens[b]]), each.tables[b:b + 1], 400, st, _st(), q_rows=_int([0, n]), max_q=n)
+    assert st.item() == 0
+    assert torch.equal(one.codes.view(torch.uint8), each.codes.view(torch.uint8)) and torch.equal(one.scales, each.scales)
+    lens[31], st = 200, _status()                              # fewer tokens than new ones: reported, the others as before
+    E.epara_kv8_append(x[:, :3], x[:, 3:], one.codes, one.scales, _int(lens), one.tables, 400, st, _st(), q_rows=_int(rows), max_q=257)
+    assert st.item() == E.ERR_PAGE_APPEND
+    st = _status()
+    E.epara_kv8_append(x[:, :3], x[:, 3:], one.codes, one.scales, _int(lens), one.tables, 400, st, _st(), q_rows=_int(rows), max_q=100)
+    assert st.item() in (E.ERR_ROWS, E.ERR_PAGE_APPEND)
 
 
 def test_append_largest_smallest_and_zero_values(E):

@@ -64,6 +64,9 @@ def test_sizes_beyond_what_is_counted_in_32_bits(E):
     assert _norm(E, d=big, x_stride=big, resid_stride=big, resid_out_stride=big, q_stride=big) == E.E_UNSUPPORTED
     for call in (_append, _attn):
         assert call(E, max_len=big, table_stride=1 << 27) == E.E_UNSUPPORTED
+    for B, T, Hq, Hkv, q in ((1, 1 << 25, 1 << 15, 1, 1 << 25), (1 << 30, 1 << 30, 8, 2, 1 << 30), (1 << 20, 1 << 20, 1 << 14, 1 << 14, 1), (2, 2, 1 << 30, 1 << 30, 1)):
+        assert E.epara_kv8_attention_scratch_bytes(B, T, Hq, Hkv, 64, q, 4096) == 0
+        assert _attn(E, B=B, T=T, Hq=Hq, Hkv=Hkv, hd=64, max_q=q, max_len=4096, table_stride=256, q_rows=P, q_stride=(1 << 31) - 8) == E.E_UNSUPPORTED
 
 
 def _append(E, **k):
