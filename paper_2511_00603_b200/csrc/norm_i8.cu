@@ -78,16 +78,15 @@ __device__ __forceinline__ void load_gain(const bf16* p, float* g) {
   }
 }
 
-// gain[c .. c + 3] for c = 4 n - shift, out of the two aligned groups that hold them (gains outside [0, d) may be anything finite)
+// gain[c .. c + 3] for c = 4 n - shift, out of the two aligned groups that hold them; zeros outside [0, d)
 __device__ __forceinline__ void load_gain_shifted(const bf16* gain, int c, int shift, int d, float* g) {
   const int n4 = c + shift;
-  const unsigned long long one = 0x3f803f803f803f80ull;
-  const unsigned long long hi = n4 < d ? *reinterpret_cast<const unsigned long long*>(gain + n4) : one;
-  const unsigned long long lo = shift && n4 > 0 ? *reinterpret_cast<const unsigned long long*>(gain + n4 - 4) : one;
+  const unsigned long long hi = n4 < d ? *reinterpret_cast<const unsigned long long*>(gain + n4) : 0ull;
+  const unsigned long long lo = shift && n4 > 0 ? *reinterpret_cast<const unsigned long long*>(gain + n4 - 4) : 0ull;
   const int s = 16 * (4 - shift);
   const unsigned long long v = shift ? lo >> s | hi << (64 - s) : hi;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) g[e] = __uint_as_float((uint32_t)(v >> (16 * e)) << 16);
+  for (int e = 0; e < 4; ++e) g[e] = c + e >= 0 && c + e < d ? __uint_as_float((uint32_t)(v >> (16 * e)) << 16) : 0.f;
 }
 
 // The row's sum of squares (without gain 0; NaN when an element is not finite) and largest magnitude to its scale and the factor of its
@@ -286,7 +285,7 @@ __global__ void __launch_bounds__(1024) rms_norm_i8_long_kernel(const NormI8 a) 
 
 template <int V, int NV, bool F32, bool PHASE>
 cudaError_t launch_as(const NormI8& a, int tpr, int per_block, cudaStream_t st) {
-  const dim3 grid((unsigned)((a.rows + per_block - 1) / per_block)), block((unsigned)(tpr * per_block));
+  const dim3 grid((unsigned)(((long long)a.rows + per_block - 1) / per_block)), block((unsigned)(tpr * per_block));
   return a.resid != nullptr ? launch_pdl(rms_norm_i8_kernel<V, NV, F32, true, PHASE>, grid, block, 0, st, a, tpr)
                             : launch_pdl(rms_norm_i8_kernel<V, NV, F32, false, PHASE>, grid, block, 0, st, a, tpr);
 }

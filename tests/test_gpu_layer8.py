@@ -81,6 +81,16 @@ def test_norm(E, rows, d, x_type, resid):
         _check_norm(x, keep, gain, q, s, r)
 
 
+@pytest.mark.parametrize("d", [1023, 4095, 4097, 90])
+def test_norm_does_not_see_what_stands_behind_the_gain(E, d):
+    rows, room = 300, torch.full((d + 8,), math.nan, dtype=torch.bfloat16, device="cuda")
+    room[:d] = (1 + 0.3 * torch.randn((d,), generator=_gen(d), device="cuda")).to(torch.bfloat16)
+    x = torch.randn((rows, d), generator=_gen(d + 1), device="cuda")
+    q, s = torch.empty((rows, d), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    E.epara_rms_norm_i8(x, room[:d], q, s, _st())
+    _check_norm(x, None, room[:d], q, s, None)
+
+
 @pytest.mark.parametrize("d", [64, 4096, 1001])
 def test_norm_strides_and_what_stands_beside(E, d):
     rows, g = 37, _gen(d)
