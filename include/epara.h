@@ -392,15 +392,15 @@ size_t epara_static_scratch_bytes(void);
  * Calls in the order of a layer: epara_rms_norm_i8 (activations to int8), epara_gemm_i8 (Wqkv), epara_kv8_append, epara_kv8_attention,
  * epara_rms_norm_i8 without gain (quantises the attention's output), epara_gemm_i8 (Wo into the residual stream), and the same pair of
  * calls around the MLP.  They launch kernels on the given stream and nothing else: no allocation, no copy, no synchronisation, so
- * they can be captured into CUDA graphs.  Every argument may be what the call before wrote.  `device` is current during the call only.
+ * they can be captured into CUDA graphs.  Every argument may be what the call before wrote; outputs overlap no input but where it says so.  `device` is current during the call only.
  * `status`: device int32 which the caller clears and a kernel sets to a code of epara_output.device_error when it finds something wrong
  * (the access is skipped, the affected outputs must not be used); no call clears it, calls may share it. */
 enum { EPARA_T_BF16 = 0, EPARA_T_F32 = 1 };
 
 /* RMSNorm of x plus residual into int8 with a scale per row:
  *   h = x + resid;  y = h * gain / sqrt(mean(h^2) + eps);  scales[row] = max(max|y| / 127, 2^-126);  q = round(y / scale).
- * x [rows, x_stride] bf16 or fp32 (x_type); resid fp32 or NULL; resid_out receives h in fp32 (NULL: not written; may be resid itself);
- * gain bf16 [d], NULL: no norm, y = h; q int8 [rows, q_stride]; strides in elements.  A row in which h, or the sum of its squares in fp32, is
+ * x [rows, x_stride] bf16 or fp32 (x_type); resid fp32 or NULL; resid_out receives h in fp32 (NULL: not written; may be resid itself; only
+ * with resid); gain bf16 [d], NULL: no norm, y = h; q int8 [rows, q_stride]; strides in elements.  A row in which h, or the sum of its squares in fp32, is
  * not finite gets a NaN scale and zero codes.  Any d up to 2^30, strides and alignment; vectors are used where d, the strides and the pointers are
  * multiples of 8 elements / 16 bytes. */
 int epara_rms_norm_i8(int device, void* cuda_stream, const void* x, int x_type, long long x_stride, const float* resid, long long resid_stride,
@@ -408,8 +408,8 @@ int epara_rms_norm_i8(int device, void* cuda_stream, const void* x, int x_type, 
                       int rows, int d);
 
 /* C = epilogue((A W^T) * a_scale[m] * w_scale[n] + bias): int8 operands, exact int32 sums, epilogues as epara_grouped_gemm.
- * K at most EPARA_GEMM_I8_MAX_K (no sum passes 31 bits) and at most 2^30 tiles of 128 x 128 outputs; beyond it UNSUPPORTED.  Rows of A and W may be read up to the next multiple of
- * 16 values, what stands behind K is ignored.  Nothing outside C's N (SwiGLU N / 2) columns is written.  A bounded wait that ran out leaves
+ * K at most EPARA_GEMM_I8_MAX_K (no sum passes 31 bits), M and N at most 2^30, at most 2^30 tiles of 128 x 128 outputs; beyond it UNSUPPORTED.
+ * Rows of A and W may be read up to the next multiple of 16 values, what stands behind K is ignored.  Nothing outside C's N (SwiGLU N / 2) columns is written.  A bounded wait that ran out leaves
  * 51..59 in *status. */
 #define EPARA_GEMM_I8_MAX_K 131071
 typedef struct {

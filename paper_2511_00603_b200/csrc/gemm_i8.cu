@@ -597,7 +597,7 @@ extern "C" int epara_gemm_i8(int device, void* cuda_stream, const epara_gemm_i8_
   if (q.M < 0 || q.N <= 0 || q.K <= 0) return EPARA_E_INVALID;
   if (q.M == 0) return EPARA_OK;                   // (whose tensors may have no address)
   if (!q.A || !q.W || !q.C || !q.a_scale || !q.w_scale) return EPARA_E_INVALID;
-  if (q.K > EPARA_GEMM_I8_MAX_K || ((long long)q.M + 127) / 128 * (((long long)q.N + 127) / 128) > 1 << 30) return EPARA_E_UNSUPPORTED;
+  if (q.K > EPARA_GEMM_I8_MAX_K || q.M > 1 << 30 || q.N > 1 << 30 || ((long long)q.M + 127) / 128 * (((long long)q.N + 127) / 128) > 1 << 30) return EPARA_E_UNSUPPORTED;
   if (q.lda % 16 || q.ldw % 16 || q.lda < q.K || q.ldw < q.K) return EPARA_E_INVALID;
   const bool f32 = (q.epilogue & EPARA_EPI_RESID_F32) != 0, swi = (q.epilogue & EPARA_EPI_SWIGLU) != 0;
   if (!aligned(q.A, 16) || !aligned(q.W, 16) || !aligned(q.C, 16) || !aligned(q.a_scale, 16) || !aligned(q.w_scale, 16)) return EPARA_E_INVALID;

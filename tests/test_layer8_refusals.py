@@ -60,6 +60,7 @@ def test_gemm_refuses(E, bad):
 def test_sizes_beyond_what_is_counted_in_32_bits(E):
     assert _gemm(E, K=E.GEMM_I8_MAX_K + 1, lda=1 << 18, ldw=1 << 18) == E.E_UNSUPPORTED          # sums past 31 bits
     assert _gemm(E, M=(1 << 31) - 1, N=1 << 20, ldc=1 << 20) == E.E_UNSUPPORTED
+    assert _gemm(E, N=(1 << 30) + 1, ldc=(1 << 31) - 1) == E.E_UNSUPPORTED and _gemm(E, M=(1 << 30) + 1) == E.E_UNSUPPORTED
     big = (1 << 30) + 8
     assert _norm(E, d=big, x_stride=big, resid_stride=big, resid_out_stride=big, q_stride=big) == E.E_UNSUPPORTED
     for call in (_append, _attn):
