@@ -431,7 +431,8 @@ int epara_gemm_i8(int device, void* cuda_stream, const epara_gemm_i8_problem* pr
  * Rows: T rows of q, k, v belong to B requests, request b to rows q_rows[b] .. q_rows[b+1] - 1 (device int32 [B + 1], not decreasing), at most
  * max_q of them (more: 103 in *status, the rows beyond are left out); q_rows NULL: one row each, T = B, max_q = 1.  kv_lens [B]: tokens
  * of the request INCLUDING its new ones, so new token i of n stands at position kv_lens[b] - n + i and attends to positions up to its own.
- * tables int32 [B, table_stride], table_stride >= ceil(max_len / 16).  max_len at most 2^30, else UNSUPPORTED.
+ * tables int32 [B, table_stride], table_stride >= ceil(max_len / 16).  max_len at most 2^30, else UNSUPPORTED; max_q, max_len, B and T decide how the
+ * work is split (nothing on the device does), so bounds close to the longest request are the fastest.
  *
  * epara_kv8_append writes k, v (bf16 [T, k_stride], [T, v_stride], kv head h at column h*hd; keys already rotated) to their slots, in pages
  * that no other request of the call appends to.  The scale of a (page, K|V, head) becomes the smallest power of two that brings

@@ -423,6 +423,44 @@ def test_attention_of_short_and_long_requests_in_one_call(E, hd, Hkv, G, ns, see
 
 
 @pytest.mark.parametrize("hd", [64, 128])
+def test_captured_call_follows_the_rows_on_the_device(E, hd):
+    """One graph, replayed with other requests long and short, other lengths, and fewer rows than it was captured for: the eager calls' bits."""
+    B, T, G, max_q = 6, 420, 4, 300
+    c = Cache(B, 20000, 2, hd, 9, used=3000)
+    q = torch.randn((T, 8 * hd), generator=_gen(9), device="cuda").to(torch.bfloat16)
+    k = torch.randn((T, 4, hd), generator=_gen(10), device="cuda").to(torch.bfloat16)
+    rows, lens, st, out = _int([0] * (B + 1)), _int([1] * B), _status(), torch.empty((T, 8 * hd), dtype=torch.bfloat16, device="cuda")
+    need = E.epara_kv8_attention_scratch_bytes(B, T, 8, 2, hd, max_q, 20000)
+    scratch = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+
+    def calls():
+        E.epara_kv8_append(k[:, :2], k[:, 2:], c.codes, c.scales, lens, c.tables, 20000, st, _st(), q_rows=rows, max_q=max_q)
+        E.epara_kv8_attention(q, c.codes, c.scales, lens, c.tables, out, 8, 2, hd, 20000, scratch, st, _st(), q_rows=rows, max_q=max_q)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        calls()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        calls()
+    for ns, now in (([1, 300, 1, 1, 1, 116], [900, 2900, 17, 1, 300, 700]), ([300, 0, 4, 5, 100, 0], [300, 50, 2500, 2500, 1000, 9]), ([1] * 6, [10, 20, 3000, 1, 2, 16])):
+        rows.copy_(_rows(ns)[0])
+        lens.copy_(_int(now))
+        codes, scales = c.codes.clone(), c.scales.clone()
+        out.fill_(55)
+        calls()
+        want, want_codes = out.clone(), c.codes.clone()
+        c.codes.copy_(codes), c.scales.copy_(scales)
+        out.fill_(55)
+        g.replay()
+        assert st.item() == 0 and torch.equal(out, want) and torch.equal(c.codes.view(torch.uint8), want_codes.view(torch.uint8))
+        _check_attention(c, q, now, ns, G, out)
+        assert (out[sum(ns):] == 55).all()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
 def test_long_requests_cut_off_beside_short_ones(E, hd):
     ns, lens = [1, 80, 2, 50], [700, 900, 30, 1000]
     c = Cache(4, 3000, 2, hd, 3, used=1000)
