@@ -99,16 +99,19 @@ __device__ __forceinline__ float row_scale(const NormI8& a, float ss, float top,
     r = 1.f / sqrtf(ss / (float)a.d + a.eps);
     fine = fine && r <= FLT_LARGEST;
   }
-  top *= r;
-  fine = fine && top <= FLT_LARGEST;
-  scale = fine ? fmaxf(top / 127.f, TINY_SCALE) : __int_as_float(0x7fffffff);
-  factor = fine ? r / scale : 0.f;
+  const float y = top * r;
+  fine = fine && y <= FLT_LARGEST;
+  scale = fine ? fmaxf(y / 127.f, TINY_SCALE) : __int_as_float(0x7fffffff);
+  // (r / scale with one rounding instead of four: a code whose y / scale lies next to a border is wrong less often)
+  factor = !fine ? 0.f : scale > TINY_SCALE ? 127.f / top : r / scale;
   if (!(factor > FLT_LARGEST)) return 1.f;
   factor = 1.f / scale;
   return r;
 }
-// y f + 1.5 x 2^23 has rn(y f) in its low bits.  (A NaN times a factor of 0 is one still: a row that is not finite has its codes masked.)
-__device__ __forceinline__ uint32_t code_of(float y, float factor) { return __float_as_uint(fmaf(y, factor, 12582912.f)); }
+// y f + 1.5 x 2^23 has rn(y f) in its low bits.  The product is rounded first: values in bf16 often lie on a border exactly, as half of the
+// largest one does, and there the rounded product is on it, too, and goes to the even code, where the factor's own error would decide otherwise.
+// (A NaN times a factor of 0 is one still: a row that is not finite has its codes masked.)
+__device__ __forceinline__ uint32_t code_of(float y, float factor) { return __float_as_uint(__fadd_rn(__fmul_rn(y, factor), 12582912.f)); }
 
 // TPR threads of a block share a row; each has NV groups of V values.
 // PHASE: rows of any length and place, V = 4.  All tensors have the same row stride, so that groups of four that are aligned in one are in
