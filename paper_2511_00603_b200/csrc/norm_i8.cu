@@ -295,9 +295,10 @@ cudaError_t launch_as(const NormI8& a, int tpr, int per_block, cudaStream_t st) 
 
 // Threads to a row: with no more rows than SMs as many as it has groups, one load of each operand deep; otherwise one to four groups a
 // thread, whichever leaves the fewest idle, more groups ahead, the more so the fewer bytes a group is.  Short rows share a warp.
-// Bytes a second on a B200, rows of 4096: x in fp32 with a residual 6.7 TB/s, in bf16 6.1; bf16 alone 4.3 (47 us for 16384 rows, floor 31: the
-// reductions of a row take as long as its loads; rows one after the other in a block, the next one requested ahead, 55); 65536 rows of 64 5.8
-// with a residual (2.1 before short rows shared a warp); 16384 rows of 4095 5.3, element by element 2.4; 6000 of 11000 5.9.
+// Bytes a second on a B200, rows of 4096: x in fp32 with a residual 6.7 TB/s, in bf16 6.4; bf16 alone 4.1 (49 us for 16384 rows, 40 without
+// gains, floor 31: some 20 instructions an element); 65536 rows of 64 5.9 with a residual (2.1 before short rows shared a warp); 16384 rows of 4095
+// 5.0, element by element 2.4; 6000 of 11000 5.6.  Tried for bf16 alone: 8 groups a thread 56, values packed until they are used 69, rows in turn
+// with the next ones on their way through shared memory 63, two values an instruction 49 (and slower for 14336 wide).
 template <int V, bool F32, bool PHASE>
 cudaError_t launch_norm_i8(const NormI8& a, int sm_count, cudaStream_t st) {
   const int groups = (a.d + V - 1) / V + (PHASE ? 1 : 0);            // (PHASE: a row may touch one more)
