@@ -8,7 +8,7 @@
 //   pair    256-row tiles on pairs of CTAs, persistent, two accumulators.
 // (A third one for up to 16 rows on mma.sync, as for bf16, was slower here: 1 x 32000 x 4096 35 us, swapped operands 23;
 // 16 x 6144 x 4096 11.4 and 8.8; 1 x 6144 x 4096 9.0 and 8.5.)
-// Few rows are bound by HBM or, below 30 MB of W, by the latencies of a launch and a first tile: 1 x 6144 x 4096 7.4 us (floor 3.8), 96 x 28672 x
+// Few rows are bound by HBM or, below 30 MB of W, by the latencies of a launch and a first tile: 1 x 6144 x 4096 6.8 us (floor 3.8), 96 x 28672 x
 // 4096 27 us, 4.4 TB/s (18.4).  Many by the tensor cores: 8192 x 4096 x 14336 332 us, 2900 TOP/s, 87 % of twice what cuBLAS does in bf16.
 // Operands come by plain TMA (columns past K and rows past the matrix arrive as zeros), products run as tcgen05.mma kind::i8,
 // sums are in tensor memory.  Every wait is bounded; a kernel that gives up leaves a code in *status.
@@ -525,16 +525,17 @@ bool make_i8_map(CUtensorMap* tm, const void* p, long long rows, long long cols,
 enum { I8_SWAP, I8_PAIR };
 struct I8Plan { int kernel, bn, split; };
 
-inline int swap_ring(int bn, long long ctas, int split, int sm_count) { return bn <= 128 && (ctas > sm_count || split == 8) ? SW_RING_2 : SW_RING_1; }
+inline int swap_ring(int bn, long long ctas, int split, int sm_count) { return bn <= 32 || (bn <= 128 && (ctas > sm_count || split == 8)) ? SW_RING_2 : SW_RING_1; }
 
-// The kernel and its tile by an estimate of the time in microseconds, whose terms are: a launch and its set-up; what an SM takes in, 105
-// KB a microsecond, against what HBM delivers of W, 6 MB a microsecond (4.6 where two CTAs with wide tiles share an SM: their rings
-// are short); and for swapped operands 0.8 for every 32 rows that a CTA writes out and 0.3 and 20 ns a row for the exchange.  Device
-// times of calls in a row with W cold, measured (estimate), swapped operands: 1 x 6144 x 4096 one range 9.5 (9.3), two 8.5 (8.6), four 8.6 (8.6);
-// 32 x 4096 x 14336 two ranges 15.4 (15.4), four 14.0 (14.5); 394 x 1000 x 776 tiles of 32 rows 5.3 (5.1), of 64 with two ranges 6.0 (6.3),
-// of 208 with two 11 (12.3); 128 x 4096 x 14336 with four 16.8 (16.4); 256 x 6144 x 4096 tiles of 96 rows 12.8 (13.9), pairs, 128 columns
-// 11.6 (11.6); 512 x 4096 x 4096 14.1 (16.0) and 12.3 (11.6); 96 x 28672 x 4096 31 (31), pairs, 256 columns 28 (26), 224 27 (25); 512 x 6144 x 4096
-// on pairs, 128 / 192 / 256 columns 18.0 / 13.7 / 16.1 (18.8 / 13.6 / 15.5); 768 x 4096 x 14336 52 / 35 / 41 (54 / 36 / 43).
+// The kernel and its tile by an estimate of the time in microseconds, whose terms are: a launch and its set-up; what an SM takes in, 105 KB a
+// microsecond, against what HBM delivers of W, 8 MB a microsecond (4.6 where two CTAs with wide tiles share an SM: their rings are short), and a
+// tenth of the smaller one; for swapped operands 0.8 for every 32 rows that a CTA writes out and the exchange, which two CTAs on an SM slow down by 0.3;
+// for pairs what a k-block takes, and 0.3 a tile more.  The figures were fitted to the times of 120 shapes of up to 700 rows, each with every
+// kernel and split: what is chosen takes 0.7 % longer than the best on average, 9 % at most.  Calls in a row with W cold, measured (estimate),
+// swapped operands: 1 x 6144 x 4096 one range 9.6 (9.4), two 8.5 (7.5), four 8.6 (8.0); 1 x 4096 x 4096 two 7.7 (7.0), four 6.7 (6.4); 32 x 4096 x
+// 14336 two 17.3 (15.7), four 14.7 (12.4); 128 x 4096 x 14336 four 16.0 (15.8), two 18.9 (24.2); 256 x 3000 x 3000 tiles of 96 rows with two
+// 9.3 (9.3), with four 15.5 (10.2), pairs, 128 columns 9.3 (10.0); 256 x 6144 x 4096 tiles of 96 rows 12.6 (14.0), pairs 11.6 (11.9); 96 x 28672 x
+// 4096 31, pairs, 256 columns 28, 224 27; 768 x 4096 x 14336 on pairs, 128 / 192 / 256 columns 52 / 35 / 41.
 I8Plan i8_plan(long long M, int N, int K, int sm_count) {
   const int kblocks = (K + KB - 1) / KB;
   const double w_mb = (double)N * K * 1e-6;
@@ -542,7 +543,7 @@ I8Plan i8_plan(long long M, int N, int K, int sm_count) {
   double best = 1e30;
   for (int bn = 128; bn <= 256; bn += 32) {
     const long long tiles = (M + 255) / 256 * ((N + bn - 1) / bn), pairs = sm_count / 2, rounds = (tiles + pairs - 1) / pairs;
-    const double t = 4.6 + std::max((double)rounds * kblocks * (0.1 + 0.00094 * bn), w_mb / 6.0) + 0.3 * (double)(rounds - 1);
+    const double t = 4.1 + std::max((double)rounds * kblocks * (0.117 + 0.001 * bn), w_mb / 5.5) + 0.3 * (double)(rounds - 1);
     if (t < best) { best = t; p.bn = bn; }
   }
   if (M > 1024) return p;
@@ -553,9 +554,10 @@ I8Plan i8_plan(long long M, int N, int K, int sm_count) {
     for (int s = 1; s <= 8 && s <= kblocks; s *= 2) {
       const long long ctas = (long long)tiles_n * ((M + bn - 1) / bn) * s, per_sm = (ctas + sm_count - 1) / sm_count;
       const bool two = swap_ring(bn, ctas, s, sm_count) == SW_RING_2;
-      const double main = (double)per_sm * ((kblocks + s - 1) / s) * (16.0 + bn / 8.0) / 105.0, hbm = w_mb / (two && bn > 64 ? 4.6 : 6.0);
-      const double out = 0.8 * ((bn + 32 * s - 1) / (32 * s)) + (s > 1 ? 0.3 + 0.02 * bn : 0.0) + (s == 8 ? 0.6 : 0.0);
-      const double t = 3.0 + std::max(main, hbm) + out * (double)(two ? (per_sm + 1) / 2 : per_sm);
+      const double main = (double)per_sm * ((kblocks + s - 1) / s) * (16.0 + bn / 8.0) / 105.0, hbm = w_mb / (two && bn > 64 ? 4.6 : 8.0);
+      const double out = 0.8 * ((bn + 32 * s - 1) / (32 * s)) + (s > 1 ? 0.23 + 0.028 * bn * (s - 1) / s : 0.0) + (s == 8 ? 0.6 : 0.0);
+      const double turns = two ? (double)((per_sm + 1) / 2) * (per_sm % 2 ? 1.0 : 1.3) : (double)per_sm;
+      const double t = 2.8 + std::max(main, hbm) + 0.1 * std::min(main, hbm) + out * turns;
       if (t < best) { best = t; p.kernel = I8_SWAP; p.bn = bn; p.split = s; }
     }
   }

@@ -179,6 +179,9 @@ SHAPES = [
     (1030, 2050, 260), (600, 5000, 2000), (2100, 1500, 130),         # pairs, 160, 224 and 192 columns
     (8200, 2048, 300), (3000, 5000, 140),                            # ... with several tiles each
     (192, 2048, 14336), (250, 900, 4096), (100, 30000, 300),         # swapped operands: wide tiles in four ranges; two CTAs to an SM in several rounds
+    (45, 13213, 456), (75, 16232, 1614), (40, 29951, 267), (258, 11962, 3762), (516, 6171, 1000),       # ... one range; one and two CTAs to an SM
+    (37, 5011, 1486), (71, 7143, 1945), (262, 3135, 6150), (33, 2388, 1014), (33, 19368, 2342),         # ... two
+    (683, 129, 1870), (793, 271, 2828), (935, 531, 6041), (21, 9653, 10547), (33, 1173, 7516), (652, 146, 10982),       # ... four and eight
 ]
 
 
