@@ -432,6 +432,8 @@ _x_types = _XTypes()
 def epara_rms_norm_i8(x, gain, q, scales, stream_ptr: int, resid=None, resid_out=None, eps: float = 1e-5, device: Optional[int] = None):
     """x [rows, d] bf16 or fp32, gain bf16 [d] or None (no norm), q int8 [rows, d], scales fp32 [rows]; resid, resid_out fp32 [rows, d] or None."""
     rows, d = x.shape
+    if d > 1 and (x.stride(1) != 1 or q.stride(1) != 1):
+        raise ValueError("the elements of a row stand next to each other")
     s = _norm_i8(x.get_device() if device is None else device, stream_ptr, x.data_ptr(), _x_types[x.dtype], x.stride(0), _ptr(resid),
                  0 if resid is None else resid.stride(0), _ptr(resid_out), 0 if resid_out is None else resid_out.stride(0), _ptr(gain), eps, q.data_ptr(), q.stride(0), scales.data_ptr(), rows, d)
     if s:
@@ -453,9 +455,12 @@ def epara_kv8_append(k, v, kv8_layer, kv_scales, kv_lens, tables, max_len: int, 
                      kv_pages: int = 0):
     """k, v: bf16 [T, Hkv, hd], the heads of a row next to each other; kv8_layer e4m3 [pages, 2, Hkv, 16, hd], kv_scales fp32 [pages, 2, Hkv];
     kv_lens int32 [B] (new tokens included), tables int32 [B, stride], q_rows int32 [B + 1] or None.  kv_pages: pages the call may touch."""
-    pages, _, Hkv, _, hd = kv8_layer.shape
+    pages, _, Hkv, slots, hd = kv8_layer.shape
+    T, heads, width = k.shape
+    if slots != 16 or heads != Hkv or width != hd or (Hkv > 1 and (k.stride(1) != hd or v.stride(1) != hd)):
+        raise ValueError("pages of 16 tokens, k and v [T, Hkv, hd] with the heads of a row next to each other")
     s = _kv8_append(k.get_device() if device is None else device, stream_ptr, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), kv8_layer.data_ptr(),
-                    kv_scales.data_ptr(), kv_pages or pages, _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), kv_lens.shape[0], k.shape[0], Hkv, hd, max_q, max_len, status.data_ptr())
+                    kv_scales.data_ptr(), kv_pages or pages, _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), kv_lens.shape[0], T, Hkv, hd, max_q, max_len, status.data_ptr())
     if s:
         _check(s, "epara_kv8_append")
 
@@ -467,8 +472,11 @@ def epara_kv8_attention_scratch_bytes(B: int, T: int, Hq: int, Hkv: int, hd: int
 def epara_kv8_attention(q, kv8_layer, kv_scales, kv_lens, tables, out, Hq: int, Hkv: int, hd: int, max_len: int, scratch, status, stream_ptr: int,
                         q_rows=None, max_q: int = 1, device: Optional[int] = None, kv_pages: int = 0):
     """q: bf16 [T, q_stride]; out bf16 [T, Hq * hd]; scratch: a tensor of epara_kv8_attention_scratch_bytes() bytes, or None where that is 0."""
+    T = q.shape[0]
+    if T > 1 and out.stride(0) != Hq * hd:
+        raise ValueError("out is [T, Hq * hd] without gaps")
     s = _kv8_attention(q.get_device() if device is None else device, stream_ptr, q.data_ptr(), q.stride(0), kv8_layer.data_ptr(),
-                       kv_scales.data_ptr(), kv_pages or kv8_layer.shape[0], _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), out.data_ptr(), kv_lens.shape[0], q.shape[0], Hq, Hkv, hd, max_q, max_len,
+                       kv_scales.data_ptr(), kv_pages or kv8_layer.shape[0], _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), out.data_ptr(), kv_lens.shape[0], T, Hq, Hkv, hd, max_q, max_len,
                        _ptr(scratch), 0 if scratch is None else scratch.nbytes, status.data_ptr())
     if s:
         _check(s, "epara_kv8_attention")

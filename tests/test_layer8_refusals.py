@@ -43,6 +43,23 @@ def test_norm_takes_no_other_type_for_bf16(E):
         E.epara_rms_norm_i8(x, None, torch.zeros((1, 8), dtype=torch.int8), torch.zeros(1), 0, device=0)
 
 
+def test_layouts_that_the_calls_cannot_see(E):
+    import torch
+    one, st = torch.zeros(1), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        E.epara_rms_norm_i8(torch.zeros((8, 4)).t(), None, torch.zeros((4, 8), dtype=torch.int8), torch.zeros(4), 0, device=0)
+    with pytest.raises(ValueError):
+        E.epara_rms_norm_i8(torch.zeros((4, 8)), None, torch.zeros((4, 16), dtype=torch.int8)[:, ::2], torch.zeros(4), 0, device=0)
+    layer, x = torch.zeros((3, 2, 4, 16, 64), dtype=torch.float8_e4m3fn), torch.zeros((2, 8, 64), dtype=torch.bfloat16)
+    for bad in (x[:, ::2], x, x[:, :4, :32]):
+        with pytest.raises(ValueError):
+            E.epara_kv8_append(bad, x[:, 4:], layer, one, st, st[None], 16, st, 0, device=0)
+    with pytest.raises(ValueError):
+        E.epara_kv8_append(x[:, :4], x[:, 4:], layer.view(6, 2, 4, 8, 64), one, st, st[None], 16, st, 0, device=0)
+    with pytest.raises(ValueError):
+        E.epara_kv8_attention(x.view(2, 512), layer, one, st, st[None], torch.zeros((2, 1024), dtype=torch.bfloat16)[:, :512], 8, 4, 64, 16, None, st, 0, device=0)
+
+
 def _gemm(E, status=P, **k):
     a = dict(A=P, W=P, a_scale=P, w_scale=P, C=P, bias=P, M=3, N=32, K=48, lda=48, ldw=48, ldc=32, epilogue=0)
     a.update(k)
