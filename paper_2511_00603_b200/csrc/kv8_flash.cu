@@ -41,6 +41,7 @@ constexpr int KF_S_WARP = 8, KF_PV_WARP = 10, KF_CONV_WARP = 12, KF_CONV_WARPS =
 constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
 constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
 constexpr float KF_RAISE = 8.0f;
+constexpr int KF_SCALE_BARRIER = 9;                   // (1 to 8: the softmax warps' turns)
 
 template <int HD>
 struct KfGeo {
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + Geo::OFF_BAR + 8 * KB_COUNT);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* const any_nan = reinterpret_cast<int*>(tmem_slot + 2);
-  float* const v_tops = reinterpret_cast<float*>(tmem_slot + 3);      // [KF_CONV_WARPS]
+  volatile float* const v_tops = reinterpret_cast<volatile float*>(tmem_slot + 3);      // [4]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // ---- the work item.  The longest ones start first: requests in order of their lengths, of each one the last rows first.  (In order of
@@ -205,25 +206,25 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  if (warp >= KF_CONV_WARP) {
-    // the largest V scale of the chunk; ids outside the pool are reported here
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  auto largest_v_scale = [&] { return fmaxf(fmaxf(fmaxf(v_tops[0], v_tops[1]), fmaxf(v_tops[2], v_tops[3])), KV8_TINY_SCALE); };
+  if (warp >= KF_S_WARP && warp < KF_CONV_WARP) {
+    // The issuers have time for the largest V scale of the chunk, which the converters need for their first V; ids outside the pool are reported here.
     float top = 0.f;
-    for (int i = threadIdx.x - KF_CONV_WARP * 32; i < n_pages; i += KF_CONV_WARPS * 32) {
+    for (int i = threadIdx.x - KF_S_WARP * 32; i < n_pages; i += (KF_CONV_WARP - KF_S_WARP) * 32) {
       const int id = page_id(i);
       if (id >= 0) top = fmaxf(top, a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh]);
       else atomicExch(a.status, ERR_PAGE_ATTEND);
     }
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-    if (lane == 0) v_tops[warp - KF_CONV_WARP] = top;
+    if (lane == 0) v_tops[warp - KF_S_WARP] = top;
+    __syncwarp();
+    asm volatile("barrier.cta.arrive.aligned %0, %1;" ::"r"(KF_SCALE_BARRIER), "r"(KF_THREADS - KF_S_WARP * 32) : "memory");
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot;
-  float v_ref = KV8_TINY_SCALE;
-#pragma unroll
-  for (int i = 0; i < KF_CONV_WARPS; ++i) v_ref = fmaxf(v_ref, v_tops[i]);
 
   bool ok = true;
   float m_ref = 0.f, l = 0.f, row_f = 0.f;            // softmax threads: the row's maximum (log2 domain), sum, score factor
@@ -277,6 +278,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     };
 #pragma unroll
     for (int j = 0; j < Geo::RAW - 1; ++j) request(j);
+    float v_ref = 1.f;
     for (int j = 0; j < steps; ++j) {
       const int slot = j % ST;
       const uint32_t parity = ((j / ST) & 1u) ^ 1u;
@@ -297,6 +299,11 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(KB_K_FULL + slot));
+      if (j == 0) {
+        __syncwarp();
+        asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(KF_SCALE_BARRIER), "r"(KF_THREADS - KF_S_WARP * 32) : "memory");
+        v_ref = largest_v_scale();
+      }
       const float vs = __shfl_sync(0xffffffffu, (j & 32) == 0 ? vs_cur : vs_next, j & 31);
       const uint32_t vf = pack_f16(vs / v_ref, vs / v_ref);
       const int t0 = t_begin + j * KF_STEP + cw * 16;
@@ -521,30 +528,31 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   }
   __syncthreads();                                    // (what the converters found is there)
   if (warp < 8 && g < n_mt && ok) {
-    // ------------------------------------------------------------------ output: a thread's row
+    // ------------------------------------------------------------------ output: a thread has a row
     tc_fence_after();
+    constexpr int PITCH = HD + 4;
+    static_assert(8 * 32 * PITCH * 4 <= Geo::OFF_NAN, "staging area");
     const uint32_t o_addr = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + KF_O_COL + g * HD;
-    const bool nans = *any_nan != 0, direct = seen <= a.chunk;
+    const bool nans = *any_nan != 0, direct = seen <= a.chunk, write = row_live && seen > t_begin;
     const size_t qr = (size_t)(row0 + rr / G) * a.Hkv * G + kvh * G + rr % G;
     bf16* const out = a.out + qr * HD;
-    float* const part = a.partial + (qr * a.max_chunks + chunk) * (HD + 2);
-    const float inv = direct ? v_ref / l : v_ref;
-    const bool write = row_live && seen > t_begin;
+    const float v_ref = largest_v_scale(), inv = direct ? v_ref / l : v_ref;
+    // Partial results leave through shared memory, which is idle now, row by row: stores of a row by each thread move 32 pieces of 8 bytes (64 tokens
+    // at the end of 4096, hd 128 35 us, like this 27).  For final rows, 16 bytes a thread, that would be the slower way (64 / 68 us).
+    const uint32_t partials = __ballot_sync(0xffffffffu, write && !direct);
+    float* const stage = reinterpret_cast<float*>(base_ptr) + warp * 32 * PITCH;
 #pragma unroll 1
     for (int c = 0; c < HD; c += 32) {
       uint32_t o[32];
       tmem_ld32(o_addr + c, o);
-      if (write) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
-        if (nans) {
+      for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
+      if (nans) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) if (nan_key[c + i] < seen) o[i] = 0x7fffffffu;
-        }
-        if (!direct) {
-#pragma unroll
-          for (int i = 0; i < 32; i += 2) __stcg(reinterpret_cast<float2*>(part + 2 + c + i), make_float2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])));
-        } else if ((reinterpret_cast<uintptr_t>(out) & 15) == 0) {
+        for (int i = 0; i < 32; ++i) if (nan_key[c + i] < seen) o[i] = 0x7fffffffu;
+      }
+      if (write && direct) {
+        if ((reinterpret_cast<uintptr_t>(out) & 15) == 0) {
 #pragma unroll
           for (int i = 0; i < 32; i += 8) {
             uint4 w;
@@ -556,10 +564,23 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
 #pragma unroll
           for (int i = 0; i < 32; ++i) out[c + i] = f2bf(__uint_as_float(o[i]));
         }
+      } else if (write) {
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(stage + lane * PITCH + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
       }
       __syncwarp();
     }
-    if (write && !direct) __stcg(reinterpret_cast<float2*>(part), make_float2(m_ref, l));
+    if (partials != 0) {
+      float* const part = a.partial + (qr * a.max_chunks + chunk) * (HD + 2);
+#pragma unroll 4
+      for (int r = 0; r < 32; ++r) {
+        if ((partials >> r & 1u) == 0) continue;
+        float* const to = reinterpret_cast<float*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(part), r)) + 2 + lane * 2;
+#pragma unroll
+        for (int k = 0; k < HD; k += 64) __stcg(reinterpret_cast<float2*>(to + k), *reinterpret_cast<const float2*>(stage + r * PITCH + k + lane * 2));
+      }
+      if (write && !direct) __stcg(reinterpret_cast<float2*>(part), make_float2(m_ref, l));
+    }
     tc_fence_before();
   }
   __syncthreads();
