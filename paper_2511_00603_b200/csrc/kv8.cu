@@ -5,6 +5,7 @@
 // keep the largest value below 448 and a tighter one would gain no precision; and when a later token of a page needs a larger
 // scale, the page's older codes are rescaled without a second rounding (but for values that become subnormal).
 #include <algorithm>
+#include <cmath>
 
 #include "../../include/epara.h"
 #include "common.cuh"
@@ -725,22 +726,38 @@ struct AttnPlan {
   int few_tokens, few_nt, few_tiles, few_chunk, few_chunks, few_clustered;         // few_tokens 0: not split
   long long many_items;                              // row tiles of the kernel for many rows
 };
-// Which kernel, by the rows of a (request, kv head): the one for many rows takes 256 at the price of one, mostly its exponentials, the other
-// one reads the cache again for every 16.  Device times, few rows and many, hd 128: 64 requests of 2048 to 4096 tokens, 32 rows 199 and 210 us,
-// 40 rows 275 and 212; 8 of them, 32 rows 33 and 42, 48 rows 50 and 44; one of 16384, 48 rows 32 and 29; one of 1000, 256 rows 20 and 32.  hd
-// 64: 64 of 2048 to 4096, 48 rows 156 and 176, 64 rows 202 and 176; one of 16384, 64 rows 23 and 24, 96 rows 28 and 25; one of 4096, 128 rows
-// 17 and 18.
-// Tiles of 8 rows or of 16: 64 requests of up to 512 tokens, 20 rows, hd 128 36 and 43 us, 32 rows 47 and 47; 64 of up to 4096, 20 rows 172 and
-// 190, 32 rows 224 and 199; 16 of up to 16384, 20 rows, hd 64 111 and 102; 32 of up to 2048, 16 rows 41 and 48; 8 of up to 4096, 16 rows 25
-// and 23.
+// Which kernel: up to 16 query rows of a (request, kv head) the one for few rows, with tiles of 8 or 16; beyond them the one whose time is
+// estimated to be the shortest.  The figures, in microseconds, were fitted to all three on 850 shapes of 12 to 2048 rows, 1 to 64 requests and 128 to
+// 65536 tokens: what is chosen takes 1.2 % longer than the best on average, the estimates are off by 14 %.  The kernel for few rows pays for tiles and for a tile's tokens,
+// the one for many for rounds of its CTAs, their steps and, with several chunks, the partial results.
+double few_us(int hd, int nt, double items, double tokens) {
+  return hd == 128 ? (nt == 1 ? 7.2 + 0.0064 * items + 3.3e-5 * items * tokens : 10.7 + 0.0136 * items + 5.2e-5 * items * tokens)
+                   : (nt == 1 ? 5.4 + 0.0041 * items + 2.0e-5 * items * tokens : 7.9 + 0.0099 * items + 2.8e-5 * items * tokens);
+}
+double many_us(int hd, double r, double steps, bool one_tile, int chunks, double rows) {
+  return hd == 128 ? 6.5 + r * (4.1 + steps * (one_tile ? 1.02 : 1.61)) + (chunks > 1 ? 1.0 + 9.0e-5 * rows * chunks : 0.0)
+                   : 4.5 + r * (2.5 + steps * (one_tile ? 0.86 : 1.18)) + (chunks > 1 ? 3.6 + 4.7e-5 * rows * chunks : 0.0);
+}
 AttnPlan attn_plan(int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len, int sm_count) {
   AttnPlan p = {};
   const int G = Hq / Hkv;
   const long long rows = (long long)max_q * G;
-  const double work = (double)rows * B * Hkv * max_len;
-  const bool many = hd == 128 ? rows > 32 && work > 3e6 : rows > 48 && work > 9e6;
-  const bool eights = rows <= 8 || (rows <= 24 && max_len <= (rows <= 16 ? 2048 : 4096)) || (rows <= 32 && max_len <= 2048 && work <= 3e6);
-  p.nt = many ? 0 : eights ? 1 : 2;
+  const int requests = std::min(std::max(T / max_q, 1), B);          // ... of that length, if all are alike
+  const int many_tiles = (int)((rows + KV8_FLASH_ROWS - 1) / KV8_FLASH_ROWS), many_chunk = kv8_flash_chunk(requests, many_tiles, Hkv, max_len, sm_count);
+  if (rows <= 16) {
+    p.nt = rows <= 8 || max_len <= 2048 ? 1 : 2;
+  } else {
+    const double tokens = std::max(max_len - 0.5 * max_q, 1.0);
+    auto few_time = [&](int nt) {
+      const double tiles = std::min((double)B * ((rows + 8 * nt - 1) / (8 * nt)), (double)T * G / (8 * nt) + B);
+      return few_us(hd, nt, tiles * Hkv, tokens);
+    };
+    const int chunks = (max_len + many_chunk - 1) / many_chunk;
+    const double steps = (chunks > 1 ? many_chunk : max_q > max_len / 2 ? tokens : (double)max_len) / 64.0;
+    const double many = many_us(hd, std::ceil((double)requests * many_tiles * Hkv * chunks / sm_count), steps, rows <= 128, chunks, (double)rows * requests * Hkv);
+    const double eights = few_time(1), sixteens = few_time(2);
+    p.nt = many < std::min(eights, sixteens) ? 0 : eights <= sixteens ? 1 : 2;
+  }
   const int tile = p.nt ? 8 * p.nt : KV8_FLASH_ROWS;
   p.tiles = (int)((rows + tile - 1) / tile);
   auto few = [&](int nt, long long tiles) { return kv8_chunks(B, (long long)B * tiles * Hkv, (nt == 1 ? 4 : 3) * sm_count, max_len); };
@@ -749,9 +766,9 @@ AttnPlan attn_plan(int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len
     p.chunk = c.tokens;
     p.clustered = c.clustered;
   } else {
-    p.chunk = kv8_flash_chunk(std::min(std::max(T / max_q, 1), B), p.tiles, Hkv, max_len, sm_count);
+    p.chunk = many_chunk;
     const int few_rows = G <= 16 ? 16 : 32;
-    if (G <= few_rows && T <= (long long)(B - 1) * max_q + few_rows / G) {             // (else none can be as short)
+    if (G <= few_rows && max_q > few_rows / G && T <= (long long)(B - 1) * max_q + few_rows / G) {             // (else none can be as short)
       p.few_tokens = few_rows / G;
       p.few_nt = G <= 8 ? 1 : 2;
       p.few_tiles = (p.few_tokens * G + 8 * p.few_nt - 1) / (8 * p.few_nt);
@@ -762,7 +779,7 @@ AttnPlan attn_plan(int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len
     }
     // every request adds at most one tile to those that the rows fill
     p.many_items = (long long)B * p.tiles;
-    if (B <= KV8_FLASH_SORTED) p.many_items = std::min(p.many_items, (long long)T * G / KV8_FLASH_ROWS + std::min(B, T / (p.few_tokens + 1)));
+    if (B <= KV8_FLASH_SORTED) p.many_items = std::min(p.many_items, (long long)T * G / KV8_FLASH_ROWS + std::max(std::min(B, T / (p.few_tokens + 1)), 1));
   }
   p.chunks = (max_len + p.chunk - 1) / p.chunk;
   return p;
