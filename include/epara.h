@@ -426,7 +426,8 @@ typedef struct {
 int epara_gemm_i8(int device, void* cuda_stream, const epara_gemm_i8_problem* problem, int* status);
 
 /* A cache layer in 8 bits: kv8_layer e4m3 [kv_pages][2 (K,V)][Hkv][16][hd], kv_scales fp32 [kv_pages][2][Hkv] (finite, not negative); a value is
- * code * scale.  hd 64 or 128, else UNSUPPORTED.
+ * code * scale.  hd 64 or 128, else UNSUPPORTED.  Attention takes V scales of a request and head within 2^100 of one another (zeros aside); an
+ * output is as exact as the tokens that its row sees, by the weight they have, allow: no other page's scale enters into it.
  *
  * Rows: T rows of q, k, v belong to B requests, request b to rows q_rows[b] .. q_rows[b+1] - 1 (device int32 [B + 1], not decreasing), at most
  * max_q of them (more: 103 in *status, the rows beyond are left out); q_rows NULL: one row each, T = B, max_q = 1.  kv_lens [B]: tokens

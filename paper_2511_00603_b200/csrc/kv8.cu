@@ -131,9 +131,11 @@ __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8
 // kv head's group); its four warps take the chunk's pages in turn, with the pages of a ring of their own in flight (16-byte
 // asynchronous copies), and are merged at the end.  The products run on mma.sync m16n8k16 in fp16, which holds every e4m3 code
 // exactly, with the query rows as the 8 columns: S^T = K Q^T (16 tokens x 8 rows), O^T += V^T P^T (16 dims x 8 rows).  Scales stay
-// out of the matrices: a page's K scale multiplies its scores, its V scale the probabilities, relative to the largest V scale
-// so far so that fp16 holds them.  Which dim a k index of the first product stands for, and which one a row of the second, is
-// free, and is chosen so that a lane reads 16 consecutive bytes of K and of V.
+// out of the matrices: a page's K scale multiplies its scores, its V scale the probabilities.  What stands in P is a weight, probability x V scale x c,
+// with a power of two c for each row that has brought the largest weight so far to at least 2^6 and lets none pass 2^15: what is 2^-20 of a
+// row's largest weight still is a normal fp16, and what a row does not see, or gives no weight, takes no bits from it.  (Relative to the largest V scale
+// instead, a page whose V is 2^26 times the others' took all of theirs.)  Which dim a k index of the first product stands for, and which one a row of the
+// second, is free, and is chosen so that a lane reads 16 consecutive bytes of K and of V.
 // Bound by HBM: 128 requests of 512 to 8192 tokens, 8 kv heads, G 4, hd 128 190 us, 6.0 TB/s (floor 175); two of 100003 and 131072 90 us,
 // 5.3 TB/s (72), one round of 536 blocks and the merge; one of a few hundred tokens 6 us, latencies.  On the tensor cores since the
 // first form, on FMAs, took 278 us for the first of these: a code and its product are three instructions there.
@@ -154,6 +156,7 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t u) {
 }
 __device__ __forceinline__ uint32_t u4(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
+constexpr float FLT_MOST = 3.4028234e38f;
 
 // Byte offset of 16-byte piece p of token r in a staged tile; placed so that the reads of a quarter warp (hd 64, V: of half a warp)
 // fall into different banks.
@@ -319,10 +322,11 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   }
 
   float o[NT][MT][4];
-  float m[NT][2], l[NT][2], v_ref = KV8_TINY_SCALE, inv_ref = 1.f / KV8_TINY_SCALE;
+  float m[NT][2], l[NT][2], wc[NT][2];             // a row's maximum (a whole number at or above it), sum, and the factor of its weights
 #pragma unroll
   for (int y = 0; y < NT; ++y) {
     m[y][0] = m[y][1] = -INFINITY;
+    wc[y][0] = wc[y][1] = __int_as_float((127 + KV8_MOST_UP) << 23);
     l[y][0] = l[y][1] = 0.f;
 #pragma unroll
     for (int j = 0; j < MT; ++j) o[y][j][0] = o[y][j][1] = o[y][j][2] = o[y][j][3] = 0.f;
@@ -336,27 +340,15 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         if (even) { id_odd = load_id(i * PP / 32 + 1); sc_odd = load_scales(id_odd); }
         else { id_even = load_id(i * PP / 32 + 1); sc_even = load_scales(id_even); }
       }
-      float top = even ? sc_even.y : sc_odd.y;
-#pragma unroll
-      for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-      if (top > v_ref) {
-        const float f = v_ref / top;
-#pragma unroll
-        for (int y = 0; y < NT; ++y)
-#pragma unroll
-          for (int j = 0; j < MT; ++j) { o[y][j][0] *= f; o[y][j][1] *= f; o[y][j][2] *= f; o[y][j][3] *= f; }
-        v_ref = top;
-        inv_ref = 1.f / top;
-      }
     }
     bool there[PP];                                // pages of the pool
-    float ks[PP], vf[PP];
+    float ks[PP], vs[PP];
 #pragma unroll
     for (int p = 0; p < PP; ++p) {
       const int at = (i * PP + p) & 31;
       there[p] = __shfl_sync(0xffffffffu, even ? id_even : id_odd, at) >= 0;
       ks[p] = __shfl_sync(0xffffffffu, even ? sc_even.x : sc_odd.x, at);
-      vf[p] = __shfl_sync(0xffffffffu, even ? sc_even.y : sc_odd.y, at) * inv_ref;
+      vs[p] = __shfl_sync(0xffffffffu, even ? sc_even.y : sc_odd.y, at);
     }
     issue(i + ST - 1);                             // into the stage that the step before this one has left
     cp_wait<ST - 1>();
@@ -394,17 +386,22 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
           for (int c = 0; c < 4; ++c) if (!there[p] || t0 + p * PAGE + gq + 8 * (c >> 1) >= seen[y][c & 1]) s[p][y][c] = -INFINITY;
       }
     }
-    // the running maximum is only raised when a score passes it by more than 2^8
+    // the running maximum is only raised when a score passes it by more than 2^8, the weights' factor only lowered when one would pass 2^15
     float top[NT][2];
     bool raise = false;
 #pragma unroll
     for (int y = 0; y < NT; ++y)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        top[y][e] = fmaxf(s[0][y][e], s[0][y][2 + e]);
+        float weight = 0.f;                        // (fmaxf drops the NaN of a row without a maximum)
+        top[y][e] = -INFINITY;
 #pragma unroll
-        for (int p = 1; p < PP; ++p) top[y][e] = fmaxf(top[y][e], fmaxf(s[p][y][e], s[p][y][2 + e]));
-        raise |= top[y][e] > m[y][e] + 8.f;
+        for (int p = 0; p < PP; ++p) {
+          const float own = fmaxf(s[p][y][e], s[p][y][2 + e]);
+          top[y][e] = fmaxf(top[y][e], own);
+          weight = fmaxf(weight, ex2(own - m[y][e]) * fminf(vs[p] * wc[y][e], FLT_MOST));
+        }
+        raise |= top[y][e] > m[y][e] + 8.f || weight > 32768.f;
       }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
@@ -413,10 +410,20 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         for (int e = 0; e < 2; ++e) {
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top[y][e] = fmaxf(top[y][e], __shfl_xor_sync(0xffffffffu, top[y][e], x));
-          if (top[y][e] > m[y][e]) {
-            const float f = ex2(m[y][e] - top[y][e]);
-            m[y][e] = top[y][e];
-            l[y][e] *= f;
+          const float to = fmaxf(m[y][e], ceilf(top[y][e])), lift = to - m[y][e];
+          float weight = 0.f;
+#pragma unroll
+          for (int p = 0; p < PP; ++p) weight = fmaxf(weight, ex2(fmaxf(s[p][y][e], s[p][y][2 + e]) - to) * vs[p]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) weight = fmaxf(weight, __shfl_xor_sync(0xffffffffu, weight, x));
+          // c times the largest weight of the step to [2^6, 2^7), unless an earlier one is larger
+          const float was = (float)((int)(__float_as_uint(wc[y][e]) >> 23) - 127);
+          const float now = fminf(fminf(was + lift, (float)(6 + 127 - (int)(__float_as_uint(weight) >> 23))), (float)KV8_MOST_UP);
+          if (to > m[y][e] || now < was) {
+            const float f = ex2(now - was - lift);
+            m[y][e] = to;
+            l[y][e] *= ex2(-lift);
+            wc[y][e] = __int_as_float((127 + (int)now) << 23);
 #pragma unroll
             for (int j = 0; j < MT; ++j) { o[y][j][e] *= f; o[y][j][2 + e] *= f; }
           }
@@ -432,8 +439,9 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         const float p0 = ex2(s[p][y][0] - m0), p1 = ex2(s[p][y][1] - m1), p2 = ex2(s[p][y][2] - m0), p3 = ex2(s[p][y][3] - m1);
         l[y][0] += p0 + p2;
         l[y][1] += p1 + p3;
-        pt[y][0] = transpose_8x8(pack_f16(p0 * vf[p], p1 * vf[p]));
-        pt[y][1] = transpose_8x8(pack_f16(p2 * vf[p], p3 * vf[p]));
+        const float v0 = fminf(vs[p] * wc[y][0], FLT_MOST), v1 = fminf(vs[p] * wc[y][1], FLT_MOST);        // (finite: a probability of zero stays one)
+        pt[y][0] = transpose_8x8(pack_f16(p0 * v0, p1 * v1));
+        pt[y][1] = transpose_8x8(pack_f16(p2 * v0, p3 * v1));
       }
       // V^T as the A operand: bytes of two tokens interleaved, then two codes at a time to fp16; k indices 2 tq + {0, 1} and + 8 are
       // those tokens, rows gq and gq + 8 of m tile j the dims gq HD / 8 + 2 j + {0, 1}
@@ -522,10 +530,11 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       const int r = 8 * y + 2 * tq + e;
+      const float back = __int_as_float(0x7f000000 - __float_as_int(wc[y][e]));              // 1 / c
       if (gq == 0) { sm_m[warp][r] = m[y][e]; sm_l[warp][r] = l[y][e]; }
 #pragma unroll
       for (int j = 0; j < MT; ++j)
-        *reinterpret_cast<float2*>(sm_o + (warp * TR + r) * HD + gq * (HD / 8) + 2 * j) = make_float2(o[y][j][e] * v_ref, o[y][j][2 + e] * v_ref);
+        *reinterpret_cast<float2*>(sm_o + (warp * TR + r) * HD + gq * (HD / 8) + 2 * j) = make_float2(o[y][j][e] * back, o[y][j][2 + e] * back);
     }
   __syncthreads();
   float* const own = sm_o + KV8_WARPS * TR * HD;                   // CLUSTER: [row][maximum, sum, dims]

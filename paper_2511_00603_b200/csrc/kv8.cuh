@@ -7,6 +7,7 @@
 namespace epara {
 
 constexpr float KV8_TINY_SCALE = 1.17549435e-38f;     // 2^-126
+constexpr int KV8_MOST_UP = 120;                      // weights -- probability x V scale -- are multiplied by at most 2^120 to make fp16 of them
 
 // two fp32 -> two e4m3 codes (lo in the low byte), nearest even, NaN to NaN
 __device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {

@@ -2,8 +2,11 @@
 //
 // A CTA takes 256 query rows of a (request, kv head) -- row = new token x query head of the group -- as two tiles of 128, and a chunk
 // of the request's keys in steps of 64 (four pages).  Everything the MMAs read is fp16, which holds an e4m3 code exactly: K and V codes
-// are converted once per CTA, Q has its rows brought to [2^14, 2^15) by powers of two.  K's page scales multiply the scores, V's scales,
-// relative to the largest of the chunk, are folded into the converted values.  Roles:
+// are converted once per CTA, Q has its rows brought to [2^14, 2^15) by powers of two.  K's page scales multiply the scores.  A V scale is 2^e times a
+// mantissa: the mantissa, 1 for the scales that the append writes, goes into the converted values, e into the exponent of the probabilities: P holds
+// weights, probability x 2^e x 2^w, with a whole number w for each row that has brought its largest weight so far to at least 2^6 and lets none pass
+// 2^15.  (With V relative to the largest scale of the chunk a page of large values took the bits of all others, from rows that did not see it, too.)  The maximum
+// is kept as a whole number: what is added to and taken from an exponent adds up without a rounding, whatever the page.  Roles:
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread per query row (at first: that row of Q into shared memory).  A row of S is read
 //                   from tensor memory once and P written over it in fp16.  The running maximum is raised, and O rescaled, only when
 //                   it grows by more than 2^8.  The warps of the two tiles on a scheduler take turns at the exponentials, so that one tile's
@@ -40,8 +43,8 @@ constexpr int KF_STEP = 64, KF_TILE = 128;
 constexpr int KF_S_WARP = 8, KF_PV_WARP = 10, KF_CONV_WARP = 12, KF_CONV_WARPS = 4;
 constexpr int KF_THREADS = 32 * (KF_CONV_WARP + KF_CONV_WARPS);
 constexpr int KF_Q_HALF = KF_TILE * 128, KF_KV_HALF = KF_STEP * 128;          // bytes of 64 columns of a tile
-constexpr float KF_RAISE = 8.0f;
-constexpr int KF_SCALE_BARRIER = 9;                   // (1 to 8: the softmax warps' turns)
+constexpr float KF_RAISE = 8.0f, KF_MOST = 15.0f;    // log2: of a probability, of a weight
+constexpr int KF_INFO = 8;                            // steps whose scales are kept: at most STAGES + 2 are between a converter and the softmax
 
 template <int HD>
 struct KfGeo {
@@ -52,8 +55,10 @@ struct KfGeo {
   static constexpr int OFF_KV = 2 * Q_BYTES;
   static constexpr int OFF_RAW = OFF_KV + STAGES * 2 * KV_BYTES;
   static constexpr int OFF_NAN = OFF_RAW + KF_CONV_WARPS * RAW * RAW_BYTES;    // first key with a NaN in V, per dim
-  static constexpr int OFF_BAR = OFF_NAN + HD * 4;
+  static constexpr int OFF_INFO = OFF_NAN + HD * 4;                            // K scales of a step's four pages, exponents of their V scales
+  static constexpr int OFF_BAR = OFF_INFO + KF_INFO * 32;
   static constexpr int SMEM = 1024 + OFF_BAR + 512;
+  static_assert(STAGES + 2 < KF_INFO, "a step's scales stay until they are read");
   static_assert(SMEM <= 227 * 1024 && 2 * SMEM > 227 * 1024, "one CTA, which takes all of the tensor memory, to an SM");
 };
 constexpr int KF_S_COL = 0, KF_O_COL = 256;          // TMEM columns: S / P buffers 0, 1 of tile 0, of tile 1; O_0, O_1
@@ -90,19 +95,15 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 __device__ __forceinline__ float kf_max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-__device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
+// a (hi + lo), rounded once but for what lo's own product loses
+__device__ __forceinline__ uint32_t hscale2(uint32_t a, uint32_t hi, uint32_t lo) {
   uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  asm("{\n\t.reg .b32 t;\n\tmul.rn.f16x2 t, %1, %3;\n\tfma.rn.f16x2 %0, %1, %2, t;\n\t}" : "=r"(r) : "r"(a), "r"(hi), "r"(lo));
   return r;
 }
 
@@ -111,11 +112,16 @@ __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ void turn_wait(int warp) { asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(1 + warp) : "memory"); }
 __device__ __forceinline__ void turn_pass(int warp) { asm volatile("barrier.cta.arrive.aligned %0, 64;" ::"r"(1 + (warp ^ 4)) : "memory"); }
 
-// The exponents are score x factor - maximum, fused, and the maximum is rounded: beyond 2^27 the largest score would stand more than 2^4
-// above or below its own maximum.  A row with such a maximum has score and maximum scaled down to 2^26 by a power of two: neighbouring fp32
-// scores are then still 4 apart, equal ones have equal weights and others next to none, as they should.
+// The exponents are score x factor - maximum, fused.  Beyond 2^22 a row has score and maximum scaled down to [2^21, 2^22) by a power of two: whole numbers
+// that the exponent of a V scale can be added to; the scores' own sums are not as exact as that.  Equal scores have equal weights, others next to none, as
+// they should.
 __device__ __forceinline__ float scale_down(float m) {
-  return fabsf(m) > 134217728.f ? __uint_as_float((280u - (__float_as_uint(fabsf(m)) >> 23)) << 23) : 1.f;
+  return fabsf(m) > 4194304.f ? __uint_as_float((275u - (__float_as_uint(fabsf(m)) >> 23)) << 23) : 1.f;
+}
+// the next whole number, scaled down, at or above m
+__device__ __forceinline__ float ceil_down(float m) {
+  const float d = scale_down(m);
+  return ceilf(m * d) / d;
 }
 
 template <int HD>
@@ -131,7 +137,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + Geo::OFF_BAR + 8 * KB_COUNT);
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* const any_nan = reinterpret_cast<int*>(tmem_slot + 2);
-  volatile float* const v_tops = reinterpret_cast<volatile float*>(tmem_slot + 3);      // [4]
+  float* const info = reinterpret_cast<float*>(base_ptr + Geo::OFF_INFO);              // [KF_INFO][K scales, V exponents][4]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // ---- the work item.  The longest ones start first: requests in order of their lengths, of each one the last rows first.  (In order of
@@ -210,24 +216,9 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
-  auto largest_v_scale = [&] { return fmaxf(fmaxf(fmaxf(v_tops[0], v_tops[1]), fmaxf(v_tops[2], v_tops[3])), KV8_TINY_SCALE); };
-  if (warp >= KF_S_WARP && warp < KF_CONV_WARP) {
-    // The issuers have time for the largest V scale of the chunk, which the converters need for their first V; ids outside the pool are reported here.
-    float top = 0.f;
-    for (int i = threadIdx.x - KF_S_WARP * 32; i < n_pages; i += (KF_CONV_WARP - KF_S_WARP) * 32) {
-      const int id = page_id(i);
-      if (id >= 0) top = fmaxf(top, a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh]);
-      else atomicExch(a.status, ERR_PAGE_ATTEND);
-    }
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-    if (lane == 0) v_tops[warp - KF_S_WARP] = top;
-    __syncwarp();
-    asm volatile("barrier.cta.arrive.aligned %0, %1;" ::"r"(KF_SCALE_BARRIER), "r"(KF_THREADS - KF_S_WARP * 32) : "memory");
-  }
 
   bool ok = true;
-  float m_ref = 0.f, l = 0.f, row_f = 0.f;            // softmax threads: the row's maximum (log2 domain), sum, score factor
+  float m_ref = 0.f, l = 0.f, row_f = 0.f, up_w = 0.f;            // softmax threads: the row's maximum (log2 domain), sum, score factor, w of its weights
   const int g = warp >> 2, row = (warp & 3) * 32 + lane, rr = r_first + g * KF_TILE + row;         // (warps 0 .. 7)
   const bool row_live = warp < 8 && g * KF_TILE + row < rows;
   const int seen = row_live ? seen0 + rr / G : 0;     // keys that the row attends to
@@ -235,9 +226,15 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
   if (warp >= KF_CONV_WARP) {
     // ------------------------------------------------------------------ converters
     const int cw = warp - KF_CONV_WARP;               // this warp's page of a step
-    int id_cur = page_id(lane * 4 + cw), id_next = page_id((lane + 32) * 4 + cw);      // of 32 steps each
-    auto scale_of = [&](int id) { return id >= 0 ? a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh] : 0.f; };
-    float vs_cur = scale_of(id_cur), vs_next = scale_of(id_next);
+    auto look_up = [&](int i) {                       // (each page of the chunk once, by one lane: ids outside the pool are reported here)
+      const int id = page_id(i);
+      if (id < 0 && i < n_pages) atomicExch(a.status, ERR_PAGE_ATTEND);
+      return id;
+    };
+    int id_cur = look_up(lane * 4 + cw), id_next = look_up((lane + 32) * 4 + cw);      // of 32 steps each
+    auto k_scale = [&](int id) { return id >= 0 ? a.scales[(size_t)id * 2 * a.Hkv + kvh] : 0.f; };
+    auto v_scale = [&](int id) { return id >= 0 ? a.scales[((size_t)id * 2 + 1) * a.Hkv + kvh] : 0.f; };
+    float ks_cur = k_scale(id_cur), ks_next = k_scale(id_next), vs_cur = v_scale(id_cur), vs_next = v_scale(id_next);
     // The pages of the next steps are requested as 16-byte asynchronous copies into a ring of this warp's own: a step is shorter than
     // the way to memory.  (By itself no faster than one step's loads in registers, 359 and 362 us for the four prompt chunks, but these
     // registers are what the conversion needs.)
@@ -266,25 +263,24 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
 #pragma unroll
       for (int x = 0; x < NX; ++x) u[x] = lds16(raw + (j % Geo::RAW) * Geo::RAW_BYTES + is_v * (EPARA_KV_PAGE * HD) + rawat[x]);
     };
-    auto put = [&](unsigned char* tile, int x, const uint4& u, bool scaled, uint32_t f) {
+    auto put = [&](unsigned char* tile, int x, const uint4& u, bool scaled, uint32_t hi2, uint32_t lo2) {
       uint4 lo = make_uint4(to_f16x2(u.x), to_f16x2(u.x >> 16), to_f16x2(u.y), to_f16x2(u.y >> 16));
       uint4 hi = make_uint4(to_f16x2(u.z), to_f16x2(u.z >> 16), to_f16x2(u.w), to_f16x2(u.w >> 16));
       if (scaled) {
-        lo.x = hmul2(lo.x, f); lo.y = hmul2(lo.y, f); lo.z = hmul2(lo.z, f); lo.w = hmul2(lo.w, f);
-        hi.x = hmul2(hi.x, f); hi.y = hmul2(hi.y, f); hi.z = hmul2(hi.z, f); hi.w = hmul2(hi.w, f);
+        lo.x = hscale2(lo.x, hi2, lo2); lo.y = hscale2(lo.y, hi2, lo2); lo.z = hscale2(lo.z, hi2, lo2); lo.w = hscale2(lo.w, hi2, lo2);
+        hi.x = hscale2(hi.x, hi2, lo2); hi.y = hscale2(hi.y, hi2, lo2); hi.z = hscale2(hi.z, hi2, lo2); hi.w = hscale2(hi.w, hi2, lo2);
       }
       *reinterpret_cast<uint4*>(tile + place[x]) = lo;
       *reinterpret_cast<uint4*>(tile + (place[x] ^ 16)) = hi;
     };
 #pragma unroll
     for (int j = 0; j < Geo::RAW - 1; ++j) request(j);
-    float v_ref = 1.f;
     for (int j = 0; j < steps; ++j) {
       const int slot = j % ST;
       const uint32_t parity = ((j / ST) & 1u) ^ 1u;
       if ((j & 31) == 0 && j > 0) {                   // the 32 steps after the next ones
-        const int id = page_id((lane + j + 32) * 4 + cw);
-        if (j & 32) { id_cur = id; vs_cur = scale_of(id); } else { id_next = id; vs_next = scale_of(id); }
+        const int id = look_up((lane + j + 32) * 4 + cw);
+        if (j & 32) { id_cur = id; ks_cur = k_scale(id); vs_cur = v_scale(id); } else { id_next = id; ks_next = k_scale(id); vs_next = v_scale(id); }
       }
       unsigned char* const kt = base_ptr + Geo::OFF_KV + slot * 2 * Geo::KV_BYTES;
       request(j + Geo::RAW - 1);                      // into the place that the step before has left
@@ -295,17 +291,22 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       fetch(j, 1, vx);
       if (j >= ST && !mbar_wait(bar(KB_K_EMPTY + slot), parity, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 23); break; }
 #pragma unroll
-      for (int x = 0; x < NX; ++x) put(kt, x, kx[x], false, 0u);
+      for (int x = 0; x < NX; ++x) put(kt, x, kx[x], false, 0u, 0u);
+      const float ks = __shfl_sync(0xffffffffu, (j & 32) == 0 ? ks_cur : ks_next, j & 31), vs = __shfl_sync(0xffffffffu, (j & 32) == 0 ? vs_cur : vs_next, j & 31);
+      const uint32_t vb = __float_as_uint(vs);
+      const float mant = vb < 0x00800000u ? vs * 8.5070592e37f : __uint_as_float((vb & 0x007fffffu) | 0x3f800000u);        // (x 2^126)
+      if (lane == 0) {
+        float* const to = info + (j % KF_INFO) * 8 + cw;
+        to[0] = ks;
+        to[4] = (float)((int)max(vb >> 23, 1u) - 127);
+      }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(KB_K_FULL + slot));
-      if (j == 0) {
-        __syncwarp();
-        asm volatile("barrier.cta.sync.aligned %0, %1;" ::"r"(KF_SCALE_BARRIER), "r"(KF_THREADS - KF_S_WARP * 32) : "memory");
-        v_ref = largest_v_scale();
-      }
-      const float vs = __shfl_sync(0xffffffffu, (j & 32) == 0 ? vs_cur : vs_next, j & 31);
-      const uint32_t vf = pack_f16(vs / v_ref, vs / v_ref);
+      const bool scaled = mant != 1.f;
+      const uint32_t mant_hi = pack_f16(mant, mant);
+      const float rest = mant - __half2float(__ushort_as_half((unsigned short)mant_hi));
+      const uint32_t mant_lo = pack_f16(rest, rest);
       const int t0 = t_begin + j * KF_STEP + cw * 16;
       uint32_t nan = 0;
 #pragma unroll
@@ -331,7 +332,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       __syncwarp();
       if (j >= ST && !mbar_wait(bar(KB_V_EMPTY + slot), parity, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 24); break; }
 #pragma unroll
-      for (int x = 0; x < NX; ++x) put(kt + Geo::KV_BYTES, x, vx[x], true, vf);
+      for (int x = 0; x < NX; ++x) put(kt + Geo::KV_BYTES, x, vx[x], scaled, mant_hi, mant_lo);
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar(KB_V_FULL + slot));
@@ -415,10 +416,6 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     const int warp_rows = min(rows - g * KF_TILE - (warp & 3) * 32, 32);       // live ones
     const int warp_r0 = r_first + g * KF_TILE + (warp & 3) * 32;
     const int seen_least = seen0 + warp_r0 / G, seen_most = warp_rows > 0 ? seen0 + (warp_r0 + warp_rows - 1) / G : 0;
-    // K scales of 32 pages, 8 steps, each: these, the next ones, and the ids of those after them, so that nobody waits for a load
-    auto k_scale = [&](int id) { return id >= 0 ? a.scales[(size_t)id * 2 * a.Hkv + kvh] : 0.f; };
-    float ks_cur = k_scale(page_id(lane)), ks_next = k_scale(page_id(32 + lane));
-    int id_after = page_id(64 + lane);
     // (every turn is taken and passed on once a step, whatever happens; the one before tile 0's first is passed here, tile 1's last one is
     // not passed on)
     float down = 1.f;
@@ -427,10 +424,6 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     int j = 0;
     for (; j < steps && g < n_mt; ++j) {
       const int sb = j & 1, k0 = t_begin + j * KF_STEP;
-      if ((j & 7) == 0 && j > 0) { ks_cur = ks_next; ks_next = k_scale(id_after); id_after = page_id((j + 16) * 4 + lane); }
-      float f[4];
-#pragma unroll
-      for (int p = 0; p < 4; ++p) f[p] = fmaxf(row_f * __shfl_sync(0xffffffffu, ks_cur, (j & 7) * 4 + p), KV8_TINY_SCALE);
       if (!mbar_wait<false>(bar(KB_S_FULL + 2 * g + sb), (j >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 29); break; }
       tc_fence_after();
       const uint32_t addr = s_addr + sb * 64;
@@ -454,7 +447,11 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
 #pragma unroll
           for (int i = 0; i < 64; ++i) if (k0 + i >= seen) v[i] = 0xff800000u;
         }
-        float mx = -INFINITY;
+        // (the converters wrote them before they reported this step's K)
+        const float4 kq = *reinterpret_cast<const float4*>(info + (j % KF_INFO) * 8), vq = *reinterpret_cast<const float4*>(info + (j % KF_INFO) * 8 + 4);
+        const float f[4] = {fmaxf(row_f * kq.x, KV8_TINY_SCALE), fmaxf(row_f * kq.y, KV8_TINY_SCALE), fmaxf(row_f * kq.z, KV8_TINY_SCALE), fmaxf(row_f * kq.w, KV8_TINY_SCALE)};
+        const float ve[4] = {vq.x, vq.y, vq.z, vq.w};
+        float mx = -INFINITY, most[4];                // a page's largest score, without its factor
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
           float m0 = -INFINITY, m1 = -INFINITY;
@@ -463,16 +460,39 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
             m0 = kf_max3(m0, __uint_as_float(v[i]), __uint_as_float(v[i + 1]));
             m1 = kf_max3(m1, __uint_as_float(v[i + 2]), __uint_as_float(v[i + 3]));
           }
-          mx = fmaxf(mx, fmaxf(m0, m1) * f[p]);
+          most[p] = fmaxf(m0, m1);
+          mx = fmaxf(mx, most[p] * f[p]);
         }
+        float add[4], k[4];                           // weight = 2^(score x factor + add), probability = weight x 2^-k
+        auto exponents = [&] {                        // answers the largest weight's
+          float top = -INFINITY;
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            k[p] = fminf(fmaxf(ve[p] + up_w, -64.f), 126.f);               // (weights 2^-64 below: zeros in fp16, but their probabilities count)
+            add[p] = k[p] - m_ref * down;
+            top = fmaxf(top, fmaf(most[p], fmaxf(f[p] * down, KV8_TINY_SCALE), add[p]));
+          }
+          return top;
+        };
+        auto lowered = [&](float w) {                 // w, if it is no more than what brings the step's largest weight to (2^6, 2^7]
+          float top = -INFINITY;
+#pragma unroll
+          for (int p = 0; p < 4; ++p) top = fmaxf(top, fmaf(most[p], fmaxf(f[p] * down, KV8_TINY_SCALE), -m_ref * down) + ve[p]);
+          return fminf(fminf(w, 7.f - ceilf(top)), (float)KV8_MOST_UP);
+        };
         if (j == 0) {
-          m_ref = mx == -INFINITY ? 0.f : mx;         // (a row that sees a key of the chunk sees its first one)
+          m_ref = mx == -INFINITY ? 0.f : ceil_down(mx);         // (a row that sees a key of the chunk sees its first one)
           down = scale_down(m_ref);
-        } else if (__any_sync(0xffffffffu, row_live && mx - m_ref > KF_RAISE)) {
-          const float m_new = fmaxf(m_ref, mx), r = ex2(m_ref - m_new);
+          up_w = lowered(INFINITY);
+          exponents();
+        } else if (__any_sync(0xffffffffu, (exponents() > KF_MOST || mx - m_ref > KF_RAISE) && row_live)) {
+          const float m_new = fmaxf(m_ref, ceil_down(mx)), lift = m_new - m_ref, before = up_w;
           m_ref = m_new;
           down = scale_down(m_ref);
-          l *= r;
+          up_w = lowered(before + lift);
+          exponents();
+          const float r = ex2(up_w - before - lift);
+          l *= ex2(-lift);
           // every P V up to the step before must be complete
           if (!mbar_wait<false>(bar(KB_PV_DONE + 2 * g + (sb ^ 1)), ((j - 1) >> 1) & 1u, abort_flag)) { ok = false; if (lane == 0) atomicExch(a.status, 30); break; }
           tc_fence_after();
@@ -487,12 +507,12 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
           }
         }
         if (turns) turn_wait(warp);
-        const uint64_t nm = f2(-m_ref * down, -m_ref * down);
         uint64_t la = 0, lb = 0;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
           const float fd = fmaxf(f[p] * down, KV8_TINY_SCALE);             // (not zero: a masked score times zero is NaN)
-          const uint64_t ff = f2(fd, fd);
+          const float back = __int_as_float((__float_as_int(12582912.f - k[p]) << 23) + 0x3f800000);           // 2^-k
+          const uint64_t ff = f2(fd, fd), nm = f2(add[p], add[p]), to_p = f2(back, back);
           uint32_t h[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -500,7 +520,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
             un_f2(fma2(f2(__uint_as_float(v[16 * p + 2 * i]), __uint_as_float(v[16 * p + 2 * i + 1])), ff, nm), x, y);
             x = ex2(x);
             y = ex2(y);
-            if (i & 1) lb = add2(lb, f2(x, y)); else la = add2(la, f2(x, y));
+            if (i & 1) lb = fma2(f2(x, y), to_p, lb); else la = fma2(f2(x, y), to_p, la);
             h[i] = pack_f16(x, y);
           }
           kf_st8(addr + 8 * p, h);
@@ -536,7 +556,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
     const bool nans = *any_nan != 0, direct = seen <= a.chunk, write = row_live && seen > t_begin;
     const size_t qr = (size_t)(row0 + rr / G) * a.Hkv * G + kvh * G + rr % G;
     bf16* const out = a.out + qr * HD;
-    const float v_ref = largest_v_scale(), inv = direct ? v_ref / l : v_ref;
+    const float inv = direct ? 1.f / l : 1.f, back = __int_as_float((127 - (int)up_w) << 23);          // 2^-w
     // Partial results leave through shared memory, which is idle now, row by row: stores of a row by each thread move 32 pieces of 8 bytes (64 tokens
     // at the end of 4096, hd 128 35 us, like this 27).  For final rows, 16 bytes a thread, that would be the slower way (64 / 68 us).
     const uint32_t partials = __ballot_sync(0xffffffffu, write && !direct);
@@ -546,7 +566,7 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
       uint32_t o[32];
       tmem_ld32(o_addr + c, o);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv);
+      for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * inv * back);
       if (nans) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) if (nan_key[c + i] < seen) o[i] = 0x7fffffffu;

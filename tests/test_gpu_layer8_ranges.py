@@ -1,0 +1,170 @@
+"""The 8-bit decoder layer at the ends of its ranges: V scales far apart, scales that are no powers of two, GELU's tail, very long rows."""
+import math
+
+import pytest
+import torch
+
+from .test_gpu_layer8 import (F64, HALF_BF16, HALF_F16, HALF_F32, Cache, _append_reference, _attend, _check_norm, _gen, _int, _rows, _st, _status,
+                              _within)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def E():
+    from paper_2511_00603_b200 import build
+    build.build()
+    from paper_2511_00603_b200 import epara
+    return epara
+
+
+# ------------------------------------------------------------------------------------------------ attention
+def _check_by_weight(c, q, lens, ns, G, out, what=""):
+    """Against the definition in 64 bits, with a tolerance from what each row itself sums up: neither a token that the row does not see nor
+    one that it gives no weight makes it wider."""
+    hd, start = c.hd, 0
+    for b, (n, L) in enumerate(zip(ns, lens)):
+        rows = slice(start, start + n)
+        start += n
+        K, V = c.values(b, L)
+        page = c.tables[b, : (L + 15) // 16].long()
+        sv = c.scales[page, 1].to(F64).t().repeat_interleave(16, 1)[:, :L]              # [Hkv, L]: the scale of each token's V
+        qb = q[rows].to(F64).view(n, c.Hkv, G, hd)
+        t = torch.einsum("thgd,hld->thgl", qb, K) / math.sqrt(hd)
+        mag = torch.einsum("thgd,hld->thgl", qb.abs(), K.abs()) / math.sqrt(hd)
+        hide = (torch.arange(L, device="cuda")[None] >= (L - n + 1 + torch.arange(n, device="cuda"))[:, None])[:, None, None]
+        t, mag = t.masked_fill(hide, -math.inf), mag.masked_fill(hide, 0)
+        p = torch.softmax(t, -1)
+        o = torch.einsum("thgl,hld->thgd", p, V)
+        pv = torch.einsum("thgl,hld->thgd", p, V.abs())
+        # A probability's error: its exponent's (sums in fp32 with a truncating adder, the factor, the maximum's subtraction, exp2 of 2 ulp).  In
+        # fp16 stands probability x V scale, the largest so far in (2^6, 2^15]: half a step of it, or of the subnormals 2^-25, which is 2^-31 of the
+        # largest weight a code (up to 448, twice that with the scale's mantissa) is multiplied by.  One more half step for
+        # a V code times a mantissa that is no power of two.
+        e_p = (mag.amax(-1) * 2.0 ** -21 + 2.0 ** -20)[..., None]
+        low = 2.0 ** -31 * 896 * (p * sv[None, :, None]).amax(-1, keepdim=True) * (~hide).to(F64).sum(-1)[..., None]
+        tol = (2 * HALF_F16 + 3 * e_p) * pv + low + HALF_BF16 * (o.abs() + 3 * HALF_F16 * pv)
+        _within(out[rows].view(n, c.Hkv, G, hd), o, tol, f"{what} b={b} n={n} L={L}")
+
+
+# Short contexts; long ones, whose chunks hold many pages for each warp; so long ones that the kernel for many rows takes all beyond 16
+MAX_LENS = [320, 40000, 1 << 20]
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ns", [[1, 1, 1], [5, 2, 40], [70, 200, 33]])
+@pytest.mark.parametrize("max_len", MAX_LENS)
+def test_v_scales_far_apart(E, hd, ns, max_len):
+    """Every (page, head) with a V scale of its own between 2^-40 and 2^40: what a row sees, and with what weight, decides what counts."""
+    lens = [77, 300, 223]
+    c = Cache(3, max_len, 2, hd, 11, used=320)
+    c.scales[:, 1] = torch.exp2(torch.randint(-40, 41, c.scales[:, 1].shape, generator=_gen(3), device="cuda").float())
+    q = torch.randn((sum(ns), 8 * hd), generator=_gen(12), device="cuda").to(torch.bfloat16)
+    out, st = _attend(E, c, q, lens, ns, 4)
+    assert st.item() == 0
+    _check_by_weight(c, q, lens, ns, 4, out)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n", [2, 30, 120])
+@pytest.mark.parametrize("max_len", MAX_LENS)
+def test_an_outlier_in_v_that_a_row_does_not_see(E, hd, n, max_len):
+    """The last page's V is 2^30 times the others': only the rows that see a token of it may notice."""
+    L = 257
+    c = Cache(1, max_len, 2, hd, 13, used=320)
+    c.scales[c.tables[0, 16].long(), 1] *= 2.0 ** 30       # token 256, which the last row alone sees
+    q = torch.randn((n, 8 * hd), generator=_gen(14), device="cuda").to(torch.bfloat16)
+    out, _ = _attend(E, c, q, [L], [n], 4)
+    _check_by_weight(c, q, [L], [n], 4, out)
+    plain, _ = _attend(E, c, q[:n - 1], [L - 1], [n - 1], 4, max_q=n)          # ... and they are what they would be without it
+    _check_by_weight(c, q[:n - 1], [L - 1], [n - 1], 4, plain)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("n", [1, 4, 40])
+@pytest.mark.parametrize("far", [8.0, 40.0])
+@pytest.mark.parametrize("max_len", MAX_LENS)
+def test_an_outlier_in_v_that_gets_next_to_no_weight(E, hd, n, far, max_len):
+    """A page whose keys stand against the queries: its V, 2^40 times the others', counts by probability times value, whichever is larger."""
+    L, G = 290, 4
+    c = Cache(1, max_len, 2, hd, 15, used=320)
+    base = torch.sign(torch.randn(hd, generator=_gen(16), device="cuda"))
+    q = (base * (1 + 0.2 * torch.rand((n, 8, hd), generator=_gen(17), device="cuda"))).to(torch.bfloat16).view(n, 8 * hd)
+    at = c.tables[0, 5].long()
+    c.codes[at, 0] = (-base * 64).to(torch.float8_e4m3fn)
+    c.scales[at, 0] = far / (64 * math.sqrt(hd))           # scores of about -far
+    c.scales[at, 1] *= 2.0 ** 40
+    out, _ = _attend(E, c, q, [L], [n], G)
+    _check_by_weight(c, q, [L], [n], G, out, f"far={far}")
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ns", [[1, 1], [3, 1], [200, 90]])
+def test_v_scales_far_apart_in_long_contexts(E, hd, ns):
+    """Several chunks, whose results meet; pages far behind the first ones read."""
+    lens = [9000, 5111]
+    c = Cache(2, 9000, 2, hd, 18)
+    c.scales[:, 1] = torch.exp2(torch.randint(-30, 31, c.scales[:, 1].shape, generator=_gen(19), device="cuda").float())
+    q = torch.randn((sum(ns), 8 * hd), generator=_gen(20), device="cuda").to(torch.bfloat16)
+    out, _ = _attend(E, c, q, lens, ns, 4)
+    _check_by_weight(c, q, lens, ns, 4, out)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("lo,hi", [(-126, -100), (80, 100)])
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("max_len", MAX_LENS)
+def test_v_scales_at_the_ends(E, hd, lo, hi, n, max_len):
+    c = Cache(1, max_len, 1, hd, 21, used=320)
+    c.scales[:, 1] = torch.exp2(torch.randint(lo, hi, c.scales[:, 1].shape, generator=_gen(22), device="cuda").float())
+    q = torch.randn((n, 4 * hd), generator=_gen(23), device="cuda").to(torch.bfloat16)
+    out, _ = _attend(E, c, q, [300], [n], 4)
+    _check_by_weight(c, q, [300], [n], 4, out)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ns", [[1, 1, 1], [5, 2, 40], [70, 200, 33]])
+@pytest.mark.parametrize("max_len", MAX_LENS)
+def test_scales_that_are_no_powers_of_two(E, hd, ns, max_len):
+    """A cache that another program has written: any finite scale that is not negative, zero among them."""
+    lens = [77, 300, 223]
+    c = Cache(3, max_len, 2, hd, 24, used=320)
+    c.scales *= 1 + torch.rand(c.scales.shape, generator=_gen(25), device="cuda")
+    c.scales[c.tables[1, 2].long(), 1] = 0
+    c.scales[c.tables[2, 4].long(), 0] = 0
+    q = torch.randn((sum(ns), 8 * hd), generator=_gen(26), device="cuda").to(torch.bfloat16)
+    out, st = _attend(E, c, q, lens, ns, 4)
+    assert st.item() == 0
+    _check_by_weight(c, q, lens, ns, 4, out)
+
+
+@pytest.mark.parametrize("many", [0, 30])
+def test_large_queries_against_the_definition(E, many):
+    """Scores of some hundreds: the weights are those of few tokens."""
+    c = Cache(1, 1 << 20 if many else 200, 1, 64, 6, used=200)
+    q = (300 * torch.randn((1 + many, 4 * 64), generator=_gen(1), device="cuda")).to(torch.bfloat16)
+    out, _ = _attend(E, c, q, [33], [1 + many], 4)
+    _check_by_weight(c, q, [33], [1 + many], 4, out)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("power", [8, 20, 24, 26, 30, 60])
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("max_len", MAX_LENS)
+def test_equal_scores_have_equal_weights(E, hd, power, n, max_len):
+    """All keys alike: however large the scores, an output is the mean of V, and pages of other V scales do not change that."""
+    L = 290
+    c = Cache(1, max_len, 1, hd, 27, used=320)
+    key = (40 * torch.randn(hd, generator=_gen(28), device="cuda")).to(torch.float8_e4m3fn)
+    c.codes[:, 0] = key
+    c.scales[:, 0] = 2.0 ** -6
+    c.scales[:, 1] = torch.exp2(torch.randint(-9, 4, c.scales[:, 1].shape, generator=_gen(29), device="cuda").float())
+    q = (2.0 ** power * torch.randn((n, 4 * hd), generator=_gen(30), device="cuda")).to(torch.bfloat16)
+    out, _ = _attend(E, c, q, [L], [n], 4)
+    V = c.values(0, L)[1][0]
+    for i in range(n):
+        sees = L - n + 1 + i
+        mean, spread = V[:sees].mean(0), V[:sees].abs().mean(0)
+        # (a weight is exact but for its rounding to fp16 and the sum's roundings)
+        tol = (HALF_F16 + 2.0 ** -16) * spread + HALF_BF16 * (mean.abs() + HALF_F16 * spread)
+        assert ((out[i].to(F64).view(4, hd) - mean).abs() <= tol).all(), i
