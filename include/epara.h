@@ -407,7 +407,8 @@ int epara_rms_norm_i8(int device, void* cuda_stream, const void* x, int x_type, 
                       float* resid_out, long long resid_out_stride, const void* gain, float eps, signed char* q, long long q_stride, float* scales,
                       int rows, int d);
 
-/* C = epilogue((A W^T) * a_scale[m] * w_scale[n] + bias): int8 operands, exact int32 sums, epilogues as epara_grouped_gemm.
+/* C = epilogue((A W^T) * a_scale[m] * w_scale[n] + bias): int8 operands, exact int32 sums, epilogues as epara_grouped_gemm, but GELU within 2^-13 of
+ * its value before it is rounded, for negative arguments too (there within 2^-12 |x|).
  * K at most EPARA_GEMM_I8_MAX_K (no sum passes 31 bits), M and N at most 2^30, at most 2^30 tiles of 128 x 128 outputs; beyond it UNSUPPORTED.
  * Rows of A and W may be read up to the next multiple of 16 values, what stands behind K is ignored.  Nothing outside C's N (SwiGLU N / 2) columns is written.  A bounded wait that ran out leaves
  * 51..59 in *status. */

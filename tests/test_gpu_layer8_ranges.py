@@ -168,3 +168,38 @@ def test_equal_scores_have_equal_weights(E, hd, power, n, max_len):
         # (a weight is exact but for its rounding to fp16 and the sum's roundings)
         tol = (HALF_F16 + 2.0 ** -16) * spread + HALF_BF16 * (mean.abs() + HALF_F16 * spread)
         assert ((out[i].to(F64).view(4, hd) - mean).abs() <= tol).all(), i
+
+
+# ------------------------------------------------------------------------------------------------ product
+@pytest.mark.parametrize("M", [3, 127, 700])
+@pytest.mark.parametrize("epi", [2, 3])
+def test_gelu_to_the_end_of_its_tail(E, M, epi):
+    """x from -9 to 9: relative to the result, GELU is as good as the bf16 that it is stored in."""
+    N, K = 255, 16
+    A, W = torch.zeros((M, 16), dtype=torch.int8, device="cuda"), torch.zeros((N, 16), dtype=torch.int8, device="cuda")
+    A[:, 0] = torch.linspace(127, 1, M, device="cuda").to(torch.int8)
+    W[:, 0] = torch.arange(-127, 128, device="cuda").to(torch.int8)
+    p = dict(A=A, W=W, M=M, N=N, K=K, epilogue=epi, a_scale=torch.full((M,), 9 / 127, device="cuda"), w_scale=torch.full((N,), 1 / 127, device="cuda"),
+             bias=torch.full((N,), -0.25, device="cuda").to(torch.bfloat16), C=torch.empty((M, N), dtype=torch.bfloat16, device="cuda"))
+    st = _status()
+    E.epara_gemm_i8(p, _st(), st)
+    x = A[:, :1].to(F64) * W[:, 0].to(F64) * p["a_scale"][:, None].to(F64) * p["w_scale"].to(F64) - (0.25 if epi & 1 else 0)
+    want = 0.5 * x * torch.special.erfc(-x / math.sqrt(2))
+    # x has three roundings in fp32, an error of at most 2^-22 x 10, by which the tail changes by up to 10 times its own value; the function itself
+    # within 2^-13
+    tol = (HALF_BF16 * (1 + 2.0 ** -11) + 2.0 ** -13 + 100 * 2.0 ** -22) * want.abs()
+    _within(p["C"], want, tol, f"M={M} epi={epi}")
+
+
+def test_gelu_of_what_is_not_finite(E):
+    M, N, K = 5, 32, 16
+    for rows in (M, 700):
+        A, W = torch.ones((rows, 16), dtype=torch.int8, device="cuda"), torch.ones((N, 16), dtype=torch.int8, device="cuda")
+        W[1::2] = -1
+        a = torch.ones(rows, device="cuda")
+        a[0], a[1], a[2] = math.inf, math.nan, 1e30
+        p = dict(A=A, W=W, M=rows, N=N, K=K, epilogue=2, a_scale=a, w_scale=torch.ones(N, device="cuda"), C=torch.empty((rows, N), dtype=torch.bfloat16, device="cuda"))
+        E.epara_gemm_i8(p, _st(), _status())
+        out = p["C"].float()
+        assert (out[0, 0::2] == math.inf).all() and torch.isnan(out[0, 1::2]).all() and torch.isnan(out[1]).all()
+        assert ((out[2, 0::2] / 1.6e31 - 1).abs() < 2.0 ** -8).all() and (out[2, 1::2] == 0).all()
