@@ -203,3 +203,29 @@ def test_gelu_of_what_is_not_finite(E):
         out = p["C"].float()
         assert (out[0, 0::2] == math.inf).all() and torch.isnan(out[0, 1::2]).all() and torch.isnan(out[1]).all()
         assert ((out[2, 0::2] / 1.6e31 - 1).abs() < 2.0 ** -8).all() and (out[2, 1::2] == 0).all()
+
+
+@pytest.mark.parametrize("epi", [0, 1, 2, 3, 4, 5, 8, 9, 11])
+def test_a_row_has_the_same_bits_in_every_batch(E, epi):
+    """Whichever kernel a batch runs on, each epilogue; the fp32 stream has subnormal values among the others."""
+    M, N, K, g = 1100, 512, 1000, _gen(33)
+    ld = (K + 15) // 16 * 16
+    A, W = (torch.randint(-128, 128, (n, ld), generator=g, device="cuda", dtype=torch.int8) for n in (M, N))
+    a, w = (0.5 + torch.rand((M,), generator=g, device="cuda")) / 64, (0.5 + torch.rand((N,), generator=g, device="cuda")) / 2000
+    a[::7] = 2.0 ** -120                                   # ... and products that are subnormal
+    bias = torch.randn((N,), generator=g, device="cuda").to(torch.bfloat16)
+    bias[::3] = 0
+    cols = N // 2 if epi & 4 else N
+    C0 = torch.randn((M, cols), generator=g, device="cuda") if epi & 8 else torch.zeros((M, cols), dtype=torch.bfloat16, device="cuda")
+    if epi & 8:
+        C0[::7, ::2] = 1e-40 * torch.randn(C0[::7, ::2].shape, generator=g, device="cuda")
+    outs, st = [], _status()
+    for m in (1100, 300, 50, 12, 1):
+        C = C0[:m].clone()
+        E.epara_gemm_i8(dict(A=A, W=W, a_scale=a, w_scale=w, bias=bias, C=C, M=m, N=N, K=K, epilogue=epi), _st(), st)
+        outs.append(C)
+    for C in outs[1:]:
+        assert torch.equal(C.view(torch.int32 if epi & 8 else torch.int16), outs[0][:len(C)].view(torch.int32 if epi & 8 else torch.int16)), len(C)
+    if epi == 8:                                           # and the sum is rounded once, subnormal or not
+        acc = (A[:, :K].to(F64) @ W[:, :K].to(F64).t()).float()
+        assert torch.equal(outs[0], C0 + acc * a[:, None] * w)
