@@ -402,13 +402,14 @@ enum { EPARA_T_BF16 = 0, EPARA_T_F32 = 1 };
  * x [rows, x_stride] bf16 or fp32 (x_type); resid fp32 or NULL; resid_out receives h in fp32 (NULL: not written; may be resid itself; only
  * with resid); gain bf16 [d], NULL: no norm, y = h; q int8 [rows, q_stride]; strides in elements.  A row in which h, or the sum of its squares in fp32, is
  * not finite gets a NaN scale and zero codes.  Any d up to 2^30, strides and alignment; vectors are used where d, the strides and the pointers are
- * multiples of 8 elements / 16 bytes. */
+ * multiples of 8 elements / 16 bytes.  Other rows are read in aligned groups of four values where the strides are the same: up to three values in front of a row and behind it
+ * (x, resid, gain), within 16 bytes that hold a value of it, may be read and are ignored; nothing is written there. */
 int epara_rms_norm_i8(int device, void* cuda_stream, const void* x, int x_type, long long x_stride, const float* resid, long long resid_stride,
                       float* resid_out, long long resid_out_stride, const void* gain, float eps, signed char* q, long long q_stride, float* scales,
                       int rows, int d);
 
 /* C = epilogue((A W^T) * a_scale[m] * w_scale[n] + bias): int8 operands, exact int32 sums, epilogues as epara_grouped_gemm, but GELU within 2^-13 of
- * its value before it is rounded, for negative arguments too (there within 2^-12 |x|).
+ * its value before it is rounded, for negative arguments too (that call's error is relative to the argument).
  * K at most EPARA_GEMM_I8_MAX_K (no sum passes 31 bits), M and N at most 2^30, at most 2^30 tiles of 128 x 128 outputs; beyond it UNSUPPORTED.
  * Rows of A and W may be read up to the next multiple of 16 values, what stands behind K is ignored.  Nothing outside C's N (SwiGLU N / 2) columns is written.  A bounded wait that ran out leaves
  * 51..59 in *status. */

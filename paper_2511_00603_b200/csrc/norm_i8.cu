@@ -243,13 +243,16 @@ rms_norm_i8_kernel(const NormI8 a, int tpr) {
 }
 
 // Rows too long for registers: the row is read twice (its second time through the caches).  With resid and no resid_out the sum
-// is formed twice.
+// is formed twice.  A thread adds up to 2^20 squares: 32 at a time in fp32, these sums in 64 bits (in fp32 alone a row of 2^23 like values was off by
+// 1.3e-5, and the error grows with the row).
 template <bool F32>
 __global__ void __launch_bounds__(1024) rms_norm_i8_long_kernel(const NormI8 a) {
   __shared__ float red[2][32];
   pdl_wait();
   const long long row = blockIdx.x;
   float ss = 0.f, top = 0.f;
+  double sum = 0.;
+  int pending = 0;
   auto value = [&](int c) {
     Raw<1, F32> x;
     x.load(a.x, row * a.x_stride + c);
@@ -264,8 +267,9 @@ __global__ void __launch_bounds__(1024) rms_norm_i8_long_kernel(const NormI8 a) 
     if (a.gain != nullptr) { ss = fmaf(h, h, ss); h *= bf2f(a.gain[c]); }
     top = fmaxf(top, fabsf(h));
     ss = fmaf(h, 0.f, ss);
+    if (++pending == 32) { sum += ss; ss = 0.f; pending = 0; }
   }
-  ss = warp_sum(ss);
+  ss = warp_sum((float)(sum + ss));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;

@@ -229,3 +229,18 @@ def test_a_row_has_the_same_bits_in_every_batch(E, epi):
     if epi == 8:                                           # and the sum is rounded once, subnormal or not
         acc = (A[:, :K].to(F64) @ W[:, :K].to(F64).t()).float()
         assert torch.equal(outs[0], C0 + acc * a[:, None] * w)
+
+
+# ------------------------------------------------------------------------------------------------ norm
+@pytest.mark.parametrize("x_type,resid", [("bf16", False), ("f32", True)])
+def test_norm_of_very_long_rows(E, x_type, resid):
+    """Rows of some millions of like values, where a running fp32 sum loses a little with every addition."""
+    d = (1 << 23) + 5
+    x = torch.full((2, d), 1.1, device="cuda").to(torch.bfloat16 if x_type == "bf16" else torch.float32)
+    x[1] += 0.01 * torch.randn((d,), generator=_gen(34), device="cuda").to(x.dtype)
+    r = torch.full((2, d), 0.3, device="cuda") if resid else None
+    gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    q, s = torch.empty((2, d), dtype=torch.int8, device="cuda"), torch.empty(2, device="cuda")
+    r_out = torch.empty_like(r) if resid else None
+    E.epara_rms_norm_i8(x, gain, q, s, _st(), resid=r, resid_out=r_out)
+    _check_norm(x, r, gain, q, s, r_out)
