@@ -170,6 +170,41 @@ def test_equal_scores_have_equal_weights(E, hd, power, n, max_len):
         assert ((out[i].to(F64).view(4, hd) - mean).abs() <= tol).all(), i
 
 
+# ------------------------------------------------------------------------------------------------ append
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ns,lens", [([1, 3, 20], [8, 40, 45]), ([2, 1, 9], [16, 18, 25])])
+def test_append_to_pages_with_scales_that_are_no_powers_of_two(E, hd, ns, lens):
+    """Tokens behind others whose scale another program has chosen: larger than the new ones need, it stays and the new codes are quotients by it;
+    smaller, the older codes are rescaled by a factor that is no power of two."""
+    Hkv = 4
+    c, g = Cache(3, 64, Hkv, hd, 31, fill=0.0), _gen(32)
+    c.codes.copy_((torch.randn(c.codes.shape, generator=g, device="cuda") * 60).clamp(-448, 448).to(torch.float8_e4m3fn))
+    c.scales.copy_(torch.rand(c.scales.shape, generator=g, device="cuda") * 0.05)      # about half of them larger than 3 / 448 to the next power
+    c.scales[:, :, 0] *= 0.01                              # heads that certainly grow, and one that certainly does not
+    c.scales[:, :, 1] += 0.1
+    x = torch.randn((sum(ns), 2 * Hkv, hd), generator=g, device="cuda").to(torch.bfloat16)
+    codes, scales, st = c.codes.to(F64), c.scales.clone(), _status()
+    _, want = _append_reference(c.codes, c.scales, x[:, :Hkv], x[:, Hkv:], c.tables, lens, ns)
+    E.epara_kv8_append(x[:, :Hkv], x[:, Hkv:], c.codes, c.scales, _int(lens), c.tables, 64, st, _st(), q_rows=_rows(ns)[0], max_q=max(ns))
+    assert st.item() == 0 and torch.equal(c.scales.to(F64), want)
+    got, start, kept, grown = c.codes.to(F64), 0, 0, 0
+    for b, (n, L) in enumerate(zip(ns, lens)):
+        for pos in range((L - n) // 16 * 16, L):
+            page, slot, t = int(c.tables[b, pos // 16]), pos % 16, pos - (L - n)
+            now = want[page]                               # [2, Hkv]
+            if t >= 0:
+                exact = x[start + t].to(F64).view(2, Hkv, hd) / now[..., None]
+            else:
+                f = scales[page].to(F64) / now
+                kept, grown = kept + int((f == 1).sum()), grown + int((f < 1).sum())
+                exact = codes[page][:, :, slot] * f[..., None]
+            # the nearest code, but for a product or quotient whose own rounding in fp32 has put it on the other side of a border
+            step = torch.exp2(torch.floor(torch.log2(exact.abs().clamp(min=2.0 ** -6))) - 3)
+            assert ((got[page][:, :, slot] - exact).abs() <= 0.5 * step + HALF_F32 * exact.abs()).all()
+        start += n
+    assert kept > 0 and grown > 0                          # both were there
+
+
 # ------------------------------------------------------------------------------------------------ product
 @pytest.mark.parametrize("M", [3, 127, 700])
 @pytest.mark.parametrize("epi", [2, 3])
@@ -232,6 +267,18 @@ def test_a_row_has_the_same_bits_in_every_batch(E, epi):
 
 
 # ------------------------------------------------------------------------------------------------ norm
+@pytest.mark.parametrize("rows", [1, 5, 300])
+@pytest.mark.parametrize("d", [1, 64, 1111, 4095, 4096, 8200, 20001])
+def test_norm_of_the_fp32_stream_alone(E, rows, d):
+    """x in fp32 with gains and without a residual: the call a layer makes."""
+    g = _gen(rows + d)
+    x = torch.randn((rows, d), generator=g, device="cuda")
+    gain = (1 + 0.3 * torch.randn((d,), generator=g, device="cuda")).to(torch.bfloat16)
+    q, s = torch.empty((rows, d), dtype=torch.int8, device="cuda"), torch.empty(rows, device="cuda")
+    E.epara_rms_norm_i8(x, gain, q, s, _st())
+    _check_norm(x, None, gain, q, s, None)
+
+
 @pytest.mark.parametrize("x_type,resid", [("bf16", False), ("f32", True)])
 def test_norm_of_very_long_rows(E, x_type, resid):
     """Rows of some millions of like values, where a running fp32 sum loses a little with every addition."""
