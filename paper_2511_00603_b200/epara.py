@@ -413,29 +413,73 @@ except (ImportError, AttributeError):
     pass
 
 
-def _ptr(t):
-    return None if t is None else t.data_ptr()
+# What the C calls get are addresses: a kernel would read them as its own types, from its own device.  So a tensor of another type, device or layout is
+# refused here.  The calls look at the tensors themselves, an attribute at a time, and come to the functions below only where something is unusual: a function
+# call for each tensor costs more than the launch (6.2 to 7.4 us a call on the host; like this 5.0 to 5.6; without looking 3.9 to 4.7).
+_BF16 = _F32 = _I8 = _I32 = _CODES = None
 
 
-class _XTypes(dict):
-    def __missing__(self, dtype):
-        name = str(dtype)
-        if name not in ("torch.bfloat16", "torch.float32"):
-            raise TypeError(f"x is bf16 or fp32, not {name}")
-        self[dtype] = T_F32 if name == "torch.float32" else T_BF16
-        return self[dtype]
+def _types():
+    """(Not at import: the rest of the binding does without torch.)"""
+    global _BF16, _F32, _I8, _I32, _CODES
+    import torch
+    _BF16, _F32, _I8, _I32, _CODES = torch.bfloat16, torch.float32, torch.int8, torch.int32, (torch.float8_e4m3fn, torch.uint8)
 
 
-_x_types = _XTypes()
+def _wants(what, t, dtype, at):
+    """t has that type and lies on device `at`."""
+    if t.dtype is not dtype:
+        raise TypeError(f"{what} is {dtype}, not {t.dtype}")
+    if t.get_device() != at:
+        raise ValueError(f"{what} on another device than the call")
+
+
+def _vector(what, t, n, dtype, at):
+    """... and n elements next to each other."""
+    _wants(what, t, dtype, at)
+    if t.numel() < n or (n > 0 and not t.is_contiguous()):
+        raise ValueError(f"{what}: {n} elements next to each other")
+
+
+def _matrix(what, t, rows, cols, dtype, at):
+    """... and [rows, cols] with the elements of a row next to each other."""
+    _wants(what, t, dtype, at)
+    n, width = t.shape
+    if n < rows or width < cols or (t.stride()[1] != 1 and cols > 1):
+        raise ValueError(f"{what}: [{rows}, {cols}], the elements of a row next to each other")
 
 
 def epara_rms_norm_i8(x, gain, q, scales, stream_ptr: int, resid=None, resid_out=None, eps: float = 1e-5, device: Optional[int] = None):
     """x [rows, d] bf16 or fp32, gain bf16 [d] or None (no norm), q int8 [rows, d], scales fp32 [rows]; resid, resid_out fp32 [rows, d] or None."""
+    if _I32 is None:
+        _types()
     rows, d = x.shape
-    if d > 1 and (x.stride(1) != 1 or q.stride(1) != 1):
-        raise ValueError("the elements of a row stand next to each other")
-    s = _norm_i8(x.get_device() if device is None else device, stream_ptr, x.data_ptr(), _x_types[x.dtype], x.stride(0), _ptr(resid),
-                 0 if resid is None else resid.stride(0), _ptr(resid_out), 0 if resid_out is None else resid_out.stride(0), _ptr(gain), eps, q.data_ptr(), q.stride(0), scales.data_ptr(), rows, d)
+    at, x_type = x.get_device(), x.dtype
+    if x_type is not _BF16 and x_type is not _F32:
+        raise TypeError(f"x is bf16 or fp32, not {x_type}")
+    (x_step, x_one), (q_step, q_one), (n, width), r_step, o_step, r_at, o_at, g_at = x.stride(), q.stride(), q.shape, 0, 0, None, None, None
+    if x_one != 1:
+        _matrix("x", x, rows, d, x_type, at)
+    if q_one != 1 or n < rows or width < d or q.dtype is not _I8 or q.get_device() != at:
+        _matrix("q", q, rows, d, _I8, at)
+    if scales.dtype is not _F32 or scales.numel() < rows or not scales.is_contiguous() or scales.get_device() != at:
+        _vector("scales", scales, rows, _F32, at)
+    if gain is not None:
+        g_at = gain.data_ptr()
+        if gain.dtype is not _BF16 or gain.numel() < d or not gain.is_contiguous() or gain.get_device() != at:
+            _vector("gain", gain, d, _BF16, at)
+    if resid is not None:
+        r_at, (r_step, one), (n, width) = resid.data_ptr(), resid.stride(), resid.shape
+        if one != 1 or n < rows or width < d or resid.dtype is not _F32 or resid.get_device() != at:
+            _matrix("resid", resid, rows, d, _F32, at)
+    if resid_out is not None:
+        o_at, (o_step, one), (n, width) = resid_out.data_ptr(), resid_out.stride(), resid_out.shape
+        if one != 1 or n < rows or width < d or resid_out.dtype is not _F32 or resid_out.get_device() != at:
+            _matrix("resid_out", resid_out, rows, d, _F32, at)
+    if rows == 1:                                          # (the distance to a row that is not there may be any)
+        x_step = q_step = r_step = o_step = d + 7 & -8
+    s = _norm_i8(at if device is None else device, stream_ptr, x.data_ptr(), T_F32 if x_type is _F32 else T_BF16, x_step, r_at, r_step, o_at, o_step, g_at, eps, q.data_ptr(), q_step, scales.data_ptr(),
+                 rows, d)
     if s:
         _check(s, "epara_rms_norm_i8")
 
@@ -443,24 +487,84 @@ def epara_rms_norm_i8(x, gain, q, scales, stream_ptr: int, resid=None, resid_out
 def epara_gemm_i8(problem: Dict, stream_ptr: int, status, device: Optional[int] = None):
     """problem: dict with torch tensors A int8 [M, lda], W int8 [N, ldw], a_scale fp32 [M], w_scale fp32 [N], C, optional bias, and M, N, K, and
     optionally the epilogue flags under "epilogue" (or "epi"); status: int32 [1], see epara.h."""
+    if _I32 is None:
+        _types()
     p = problem
-    A, W, out = p["A"], p["W"], p["C"]
-    s = _gemm_i8(A.get_device() if device is None else device, stream_ptr, A.data_ptr(), W.data_ptr(), p["a_scale"].data_ptr(),
-                 p["w_scale"].data_ptr(), out.data_ptr(), _ptr(p.get("bias")), p["M"], p["N"], p["K"], A.stride(0), W.stride(0), out.stride(0), p.get("epilogue", p.get("epi", 0)), status.data_ptr())
+    A, W, out, bias, M, N, K, a_scale, w_scale = p["A"], p["W"], p["C"], p.get("bias"), p["M"], p["N"], p["K"], p["a_scale"], p["w_scale"]
+    at, epilogue, b_at = A.get_device(), p.get("epilogue", p.get("epi", 0)), None
+    (lda, one), (n, width) = A.stride(), A.shape
+    if one != 1 or n < M or width < K or A.dtype is not _I8:
+        _matrix("A", A, M, K, _I8, at)
+    (ldw, one), (n, width) = W.stride(), W.shape
+    if one != 1 or n < N or width < K or W.dtype is not _I8 or W.get_device() != at:
+        _matrix("W", W, N, K, _I8, at)
+    (ldc, one), (n, width), cols, c_type = out.stride(), out.shape, N // 2 if epilogue & EPI_SWIGLU else N, _F32 if epilogue & EPI_RESID_F32 else _BF16
+    if one != 1 or n < M or width < cols or out.dtype is not c_type or out.get_device() != at:
+        _matrix("C", out, M, cols, c_type, at)
+    if a_scale.dtype is not _F32 or a_scale.numel() < M or not a_scale.is_contiguous() or a_scale.get_device() != at:
+        _vector("a_scale", a_scale, M, _F32, at)
+    if w_scale.dtype is not _F32 or w_scale.numel() < N or not w_scale.is_contiguous() or w_scale.get_device() != at:
+        _vector("w_scale", w_scale, N, _F32, at)
+    if bias is not None:
+        b_at = bias.data_ptr()
+        if epilogue & EPI_BIAS:
+            _vector("bias", bias, N, _BF16, at)
+    if status.dtype is not _I32 or status.get_device() != at:
+        _wants("status", status, _I32, at)
+    if M == 1:
+        lda, ldc = K + 15 & -16, cols + 7 & -8
+    if N == 1:
+        ldw = K + 15 & -16
+    s = _gemm_i8(at if device is None else device, stream_ptr, A.data_ptr(), W.data_ptr(), a_scale.data_ptr(), w_scale.data_ptr(), out.data_ptr(), b_at, M, N, K, lda, ldw, ldc, epilogue, status.data_ptr())
     if s:
         _check(s, "epara_gemm_i8")
+
+
+def _cache(kv8_layer, kv_scales, kv_lens, tables, q_rows, status, pages, B, Hkv, hd, kv_pages, at):
+    """What both calls ask of the cache, the tables and the rows.  Answers the tables' row distance."""
+    if kv8_layer.dtype not in _CODES:
+        raise TypeError(f"codes are e4m3, not {kv8_layer.dtype}")
+    if kv_scales.dtype is not _F32 or kv_scales.get_device() != at:
+        _wants("kv_scales", kv_scales, _F32, at)
+    if not kv8_layer.is_contiguous() or not kv_scales.is_contiguous() or kv8_layer.numel() != pages * 32 * Hkv * hd or kv_scales.numel() != pages * 2 * Hkv:
+        raise ValueError("a layer is [pages, 2, Hkv, 16, hd] and its scales [pages, 2, Hkv], both without gaps")
+    if kv8_layer.get_device() != at or kv_pages > pages:
+        raise ValueError("more pages than the layer has, or a layer on another device than the call")
+    if kv_lens.dtype is not _I32 or kv_lens.get_device() != at or not kv_lens.is_contiguous():
+        _vector("kv_lens", kv_lens, B, _I32, at)
+    (step, one), (n, width) = tables.stride(), tables.shape
+    if one != 1 or n < B or tables.dtype is not _I32 or tables.get_device() != at:
+        _matrix("tables", tables, B, width, _I32, at)
+    if q_rows is not None:
+        if q_rows.numel() != B + 1:
+            raise ValueError("q_rows has one element more than there are requests")
+        if q_rows.dtype is not _I32 or q_rows.get_device() != at or not q_rows.is_contiguous():
+            _vector("q_rows", q_rows, B + 1, _I32, at)
+    if status.dtype is not _I32 or status.get_device() != at:
+        _wants("status", status, _I32, at)
+    return step if B > 1 else width
 
 
 def epara_kv8_append(k, v, kv8_layer, kv_scales, kv_lens, tables, max_len: int, status, stream_ptr: int, q_rows=None, max_q: int = 1, device: Optional[int] = None,
                      kv_pages: int = 0):
     """k, v: bf16 [T, Hkv, hd], the heads of a row next to each other; kv8_layer e4m3 [pages, 2, Hkv, 16, hd], kv_scales fp32 [pages, 2, Hkv];
     kv_lens int32 [B] (new tokens included), tables int32 [B, stride], q_rows int32 [B + 1] or None.  kv_pages: pages the call may touch."""
-    pages, _, Hkv, slots, hd = kv8_layer.shape
-    T, heads, width = k.shape
-    if slots != 16 or heads != Hkv or width != hd or (Hkv > 1 and (k.stride(1) != hd or v.stride(1) != hd)):
+    if _I32 is None:
+        _types()
+    pages, two, Hkv, slots, hd = kv8_layer.shape
+    shape, at, B = k.shape, k.get_device(), kv_lens.shape[0]
+    T, heads, width = shape
+    (k_step, k_head, k_one), (v_step, v_head, v_one) = k.stride(), v.stride()
+    if two != 2 or slots != 16 or heads != Hkv or width != hd or v.shape != shape or k_one != 1 or v_one != 1 or (Hkv > 1 and (k_head != hd or v_head != hd)):
         raise ValueError("pages of 16 tokens, k and v [T, Hkv, hd] with the heads of a row next to each other")
-    s = _kv8_append(k.get_device() if device is None else device, stream_ptr, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), kv8_layer.data_ptr(),
-                    kv_scales.data_ptr(), kv_pages or pages, _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), kv_lens.shape[0], T, Hkv, hd, max_q, max_len, status.data_ptr())
+    if k.dtype is not _BF16 or v.dtype is not _BF16 or v.get_device() != at:
+        _wants("k", k, _BF16, at)
+        _wants("v", v, _BF16, at)
+    table_step = _cache(kv8_layer, kv_scales, kv_lens, tables, q_rows, status, pages, B, Hkv, hd, kv_pages, at)
+    if T <= 1:
+        k_step = v_step = Hkv * hd
+    s = _kv8_append(at if device is None else device, stream_ptr, k.data_ptr(), k_step, v.data_ptr(), v_step, kv8_layer.data_ptr(), kv_scales.data_ptr(), kv_pages or pages,
+                    None if q_rows is None else q_rows.data_ptr(), kv_lens.data_ptr(), tables.data_ptr(), table_step, B, T, Hkv, hd, max_q, max_len, status.data_ptr())
     if s:
         _check(s, "epara_kv8_append")
 
@@ -472,12 +576,26 @@ def epara_kv8_attention_scratch_bytes(B: int, T: int, Hq: int, Hkv: int, hd: int
 def epara_kv8_attention(q, kv8_layer, kv_scales, kv_lens, tables, out, Hq: int, Hkv: int, hd: int, max_len: int, scratch, status, stream_ptr: int,
                         q_rows=None, max_q: int = 1, device: Optional[int] = None, kv_pages: int = 0):
     """q: bf16 [T, q_stride]; out bf16 [T, Hq * hd]; scratch: a tensor of epara_kv8_attention_scratch_bytes() bytes, or None where that is 0."""
-    T = q.shape[0]
-    if T > 1 and out.stride(0) != Hq * hd:
+    if _I32 is None:
+        _types()
+    if q.dim() != 2:
+        q = q.view(q.shape[0], q.shape[1] * q.shape[2])
+    (T, width), (q_step, one), at, pages, B = q.shape, q.stride(), q.get_device(), kv8_layer.shape[0], kv_lens.shape[0]
+    if one != 1 or width < Hq * hd or q.dtype is not _BF16:
+        _matrix("q", q, T, Hq * hd, _BF16, at)
+    if out.dtype is not _BF16 or out.get_device() != at:
+        _wants("out", out, _BF16, at)
+    if not out.is_contiguous() or out.numel() < T * Hq * hd:
         raise ValueError("out is [T, Hq * hd] without gaps")
-    s = _kv8_attention(q.get_device() if device is None else device, stream_ptr, q.data_ptr(), q.stride(0), kv8_layer.data_ptr(),
-                       kv_scales.data_ptr(), kv_pages or kv8_layer.shape[0], _ptr(q_rows), kv_lens.data_ptr(), tables.data_ptr(), tables.stride(0), out.data_ptr(), kv_lens.shape[0], T, Hq, Hkv, hd, max_q, max_len,
-                       _ptr(scratch), 0 if scratch is None else scratch.nbytes, status.data_ptr())
+    table_step, s_at, s_bytes = _cache(kv8_layer, kv_scales, kv_lens, tables, q_rows, status, pages, B, Hkv, hd, kv_pages, at), None, 0
+    if scratch is not None:
+        s_at, s_bytes = scratch.data_ptr(), scratch.nbytes
+        if scratch.get_device() != at or not scratch.is_contiguous():
+            raise ValueError("scratch on another device than the call, or with gaps")
+    if T <= 1:
+        q_step = Hq * hd
+    s = _kv8_attention(at if device is None else device, stream_ptr, q.data_ptr(), q_step, kv8_layer.data_ptr(), kv_scales.data_ptr(), kv_pages or pages, None if q_rows is None else q_rows.data_ptr(),
+                       kv_lens.data_ptr(), tables.data_ptr(), table_step, out.data_ptr(), B, T, Hq, Hkv, hd, max_q, max_len, s_at, s_bytes, status.data_ptr())
     if s:
         _check(s, "epara_kv8_attention")
 
