@@ -923,7 +923,7 @@ size_t epara_kv8_attention_scratch_bytes(int device, int B, int T, int Hq, int H
   using namespace epara;
   if (B <= 0 || T <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || hd <= 0 || max_q <= 0 || max_len <= 0) return 0;
   max_q = std::min(max_q, T);
-  if (!attn_countable(B, Hq, Hkv, max_q)) return 0;
+  if (!attn_countable(B, Hq, Hkv, max_q) || max_len > 1 << 30) return 0;          // (the call itself is UNSUPPORTED)
   const AttnPlan p = attn_plan(B, T, Hq, Hkv, hd, max_q, max_len, device_sm_count(device));
   return many_scratch(p, T, Hq, hd) + few_scratch(p, B, Hq, hd);
 }

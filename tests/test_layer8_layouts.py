@@ -182,3 +182,11 @@ def test_what_arrives(E):
     assert a[3] == 512 and a[10] == 7 and a[20] == 80
     assert _attend(E, q=qkv[:, :4])[3] == 512 and _attend(E, out=torch.zeros((3, 4, 64), dtype=bf))
     assert _attend(E, layer=torch.zeros((9, 2, 2, 16, 64), dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("max_q", [1, 64])
+@pytest.mark.parametrize("max_len", [(1 << 30) + 1, (1 << 31) - 1])
+def test_no_scratch_for_lengths_that_no_call_takes(max_q, max_len):
+    from paper_2511_00603_b200 import epara
+    assert epara.epara_kv8_attention_scratch_bytes(1, max_q, 8, 2, 128, max_q, max_len) == 0
+    assert epara.epara_kv8_attention_scratch_bytes(1, max_q, 8, 2, 128, max_q, 1 << 30) < 1 << 40
