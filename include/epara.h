@@ -411,6 +411,7 @@ int epara_rms_norm_i8(int device, void* cuda_stream, const void* x, int x_type, 
 /* C = epilogue((A W^T) * a_scale[m] * w_scale[n] + bias): int8 operands, exact int32 sums, epilogues as epara_grouped_gemm, but GELU within 2^-13 of
  * its value before it is rounded, for negative arguments too (that call's error is relative to the argument).
  * K at most EPARA_GEMM_I8_MAX_K (no sum passes 31 bits), M and N at most 2^30, at most 2^30 tiles of 128 x 128 outputs; beyond it UNSUPPORTED.
+ * A, W, C, a_scale, w_scale and bias start on 16 bytes (a part of the rows may start at any row of A; its scales at every fourth).
  * Rows of A and W may be read up to the next multiple of 16 values, what stands behind K is ignored.  Nothing outside C's N (SwiGLU N / 2) columns is written.  A bounded wait that ran out leaves
  * 51..59 in *status. */
 #define EPARA_GEMM_I8_MAX_K 131071
@@ -428,7 +429,7 @@ typedef struct {
 int epara_gemm_i8(int device, void* cuda_stream, const epara_gemm_i8_problem* problem, int* status);
 
 /* A cache layer in 8 bits: kv8_layer e4m3 [kv_pages][2 (K,V)][Hkv][16][hd], kv_scales fp32 [kv_pages][2][Hkv] (finite, not negative); a value is
- * code * scale.  hd 64 or 128, else UNSUPPORTED.  Attention takes V scales of a request and head within 2^100 of one another (zeros aside); an
+ * code * scale.  hd 64 or 128, else UNSUPPORTED.  kv8_layer, q, k and v start on 16 bytes, k_stride, v_stride and q_stride are multiples of 8.  Attention takes V scales of a request and head within 2^100 of one another (zeros aside); an
  * output is as exact as the tokens that its row sees, by the weight they have, allow: no other page's scale enters into it.
  *
  * Rows: T rows of q, k, v belong to B requests, request b to rows q_rows[b] .. q_rows[b+1] - 1 (device int32 [B + 1], not decreasing), at most
