@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   }
 
   float o[NT][MT][4];
-  float m[NT][2], l[NT][2], wc[NT][2];             // a row's maximum (a whole number at or above it), sum, and the factor of its weights
+  float m[NT][2], l[NT][2], wc[NT][2];             // a row's maximum, sum, and the factor of its weights
 #pragma unroll
   for (int y = 0; y < NT; ++y) {
     m[y][0] = m[y][1] = -INFINITY;
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
         for (int e = 0; e < 2; ++e) {
 #pragma unroll
           for (int x = 4; x < 32; x <<= 1) top[y][e] = fmaxf(top[y][e], __shfl_xor_sync(0xffffffffu, top[y][e], x));
-          const float to = fmaxf(m[y][e], ceilf(top[y][e])), lift = to - m[y][e];
+          const float to = fmaxf(m[y][e], top[y][e]), lift = to - m[y][e];
           float weight = 0.f;
 #pragma unroll
           for (int p = 0; p < PP; ++p) weight = fmaxf(weight, ex2(fmaxf(s[p][y][e], s[p][y][2 + e]) - to) * vs[p]);
@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
           for (int x = 4; x < 32; x <<= 1) weight = fmaxf(weight, __shfl_xor_sync(0xffffffffu, weight, x));
           // c times the largest weight of the step to [2^6, 2^7), unless an earlier one is larger
           const float was = (float)((int)(__float_as_uint(wc[y][e]) >> 23) - 127);
-          const float now = fminf(fminf(was + lift, (float)(6 + 127 - (int)(__float_as_uint(weight) >> 23))), (float)KV8_MOST_UP);
+          const float now = fminf(fminf(was + floorf(lift), (float)(6 + 127 - (int)(__float_as_uint(weight) >> 23))), (float)KV8_MOST_UP);
           if (to > m[y][e] || now < was) {
             const float f = ex2(now - was - lift);
             m[y][e] = to;

@@ -6,7 +6,8 @@
 // mantissa: the mantissa, 1 for the scales that the append writes, goes into the converted values, e into the exponent of the probabilities: P holds
 // weights, probability x 2^e x 2^w, with a whole number w for each row that has brought its largest weight so far to at least 2^6 and lets none pass
 // 2^15.  (With V relative to the largest scale of the chunk a page of large values took the bits of all others, from rows that did not see it, too.)  The maximum
-// is kept as a whole number: what is added to and taken from an exponent adds up without a rounding, whatever the page.  Roles:
+// is kept as a whole number where its last bit would show beside e: what is added to and taken from an exponent then adds up without a rounding, whatever the
+// page.  Roles:
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread per query row (at first: that row of Q into shared memory).  A row of S is read
 //                   from tensor memory once and P written over it in fp16.  The running maximum is raised, and O rescaled, only when
 //                   it grows by more than 2^8.  The warps of the two tiles on a scheduler take turns at the exponentials, so that one tile's
@@ -118,10 +119,11 @@ __device__ __forceinline__ void turn_pass(int warp) { asm volatile("barrier.cta.
 __device__ __forceinline__ float scale_down(float m) {
   return fabsf(m) > 4194304.f ? __uint_as_float((275u - (__float_as_uint(fabsf(m)) >> 23)) << 23) : 1.f;
 }
-// the next whole number, scaled down, at or above m
-__device__ __forceinline__ float ceil_down(float m) {
+// What a row's maximum is kept as: itself, so that the probability of its token is exactly 1, up to 2^10, where the exponent of a V scale adds to it within 2^-15;
+// beyond it the next whole number, scaled down, at or above it.
+__device__ __forceinline__ float reference(float m) {
   const float d = scale_down(m);
-  return ceilf(m * d) / d;
+  return fabsf(m) <= 1024.f ? m : ceilf(m * d) / d;
 }
 
 template <int HD>
@@ -481,15 +483,15 @@ __global__ void __launch_bounds__(KF_THREADS, 1) kv8_flash_kernel(const Kv8Attn 
           return fminf(fminf(w, 7.f - ceilf(top)), (float)KV8_MOST_UP);
         };
         if (j == 0) {
-          m_ref = mx == -INFINITY ? 0.f : ceil_down(mx);         // (a row that sees a key of the chunk sees its first one)
+          m_ref = mx == -INFINITY ? 0.f : reference(mx);         // (a row that sees a key of the chunk sees its first one)
           down = scale_down(m_ref);
           up_w = lowered(INFINITY);
           exponents();
         } else if (__any_sync(0xffffffffu, (exponents() > KF_MOST || mx - m_ref > KF_RAISE) && row_live)) {
-          const float m_new = fmaxf(m_ref, ceil_down(mx)), lift = m_new - m_ref, before = up_w;
+          const float m_new = fmaxf(m_ref, reference(mx)), lift = m_new - m_ref, before = up_w;
           m_ref = m_new;
           down = scale_down(m_ref);
-          up_w = lowered(before + lift);
+          up_w = lowered(before + floorf(lift));
           exponents();
           const float r = ex2(up_w - before - lift);
           l *= ex2(-lift);
