@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8
 // asynchronous copies), and are merged at the end.  The products run on mma.sync m16n8k16 in fp16, which holds every e4m3 code
 // exactly, with the query rows as the 8 columns: S^T = K Q^T (16 tokens x 8 rows), O^T += V^T P^T (16 dims x 8 rows).  Scales stay
 // out of the matrices: a page's K scale multiplies its scores, its V scale the probabilities.  What stands in P is a weight, probability x V scale x c,
-// with a power of two c for each row that has brought the largest weight so far to at least 2^6 and lets none pass 2^15: what is 2^-20 of a
+// with a power of two c for each row that has brought the largest weight so far to at least 2^6 and lets none pass what fp16 holds: what is 2^-20 of a
 // row's largest weight still is a normal fp16, and what a row does not see, or gives no weight, takes no bits from it.  (Relative to the largest V scale
 // instead, a page whose V is 2^26 times the others' took all of theirs.)  Which dim a k index of the first product stands for, and which one a row of the
 // second, is free, and is chosen so that a lane reads 16 consecutive bytes of K and of V.
@@ -156,7 +156,6 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t u) {
 }
 __device__ __forceinline__ uint32_t u4(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 __device__ __forceinline__ float nan_f() { return __int_as_float(0x7fffffff); }
-constexpr float FLT_MOST = 3.4028234e38f;
 
 // Byte offset of 16-byte piece p of token r in a staged tile; placed so that the reads of a quarter warp (hd 64, V: of half a warp)
 // fall into different banks.
@@ -185,10 +184,13 @@ __device__ __forceinline__ float2 ld_cluster(uint32_t addr) {
   asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
 }
+constexpr int kv8_blocks(int hd, int nt) { return nt == 1 ? 4 : hd == 64 ? 3 : 2; }
 template <int HD, int NT>
 struct Kv8Geo {
-  // pages that a warp takes at once (hd 64: what a step costs beside its products is paid for two), steps in its ring, blocks to an SM
-  static constexpr int PAGES = HD == 64 ? 2 : 1, STAGES = NT == 1 ? 3 : 4, BLOCKS = NT == 1 ? 4 : 3;
+  // pages that a warp takes at once (hd 64: what a step costs beside its products is paid for two), steps in its ring, blocks to an SM: for 16 rows of hd 128
+  // two, for in the registers of three the loop spills (32 requests of 4096 with 4 tokens each 69 us, three 95; hd 64 three 49, two 49, 64 requests with 8 tokens
+  // 128 and 157)
+  static constexpr int PAGES = HD == 64 ? 2 : 1, STAGES = NT == 1 ? 3 : 4, BLOCKS = kv8_blocks(HD, NT);
   static constexpr int RING = KV8_WARPS * STAGES * PAGES * 2 * PAGE * HD, MERGE = KV8_WARPS * 8 * NT * HD * 4;
   static constexpr int MERGED = MERGE + 8 * NT * (HD + 2) * 4, SMEM = RING > MERGED ? RING : MERGED;       // ... and the block's own result behind it
 };
@@ -322,11 +324,11 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
   }
 
   float o[NT][MT][4];
-  float m[NT][2], l[NT][2], wc[NT][2];             // a row's maximum, sum, and the factor of its weights
+  float m[NT][2], l[NT][2], wc[NT][2];             // a row's maximum so far, sum, and c
 #pragma unroll
   for (int y = 0; y < NT; ++y) {
-    m[y][0] = m[y][1] = -INFINITY;
-    wc[y][0] = wc[y][1] = __int_as_float((127 + KV8_MOST_UP) << 23);
+    m[y][0] = m[y][1] = KV8_NONE;
+    wc[y][0] = wc[y][1] = 1.f;
     l[y][0] = l[y][1] = 0.f;
 #pragma unroll
     for (int j = 0; j < MT; ++j) o[y][j][0] = o[y][j][1] = o[y][j][2] = o[y][j][3] = 0.f;
@@ -386,40 +388,48 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
           for (int c = 0; c < 4; ++c) if (!there[p] || t0 + p * PAGE + gq + 8 * (c >> 1) >= seen[y][c & 1]) s[p][y][c] = -INFINITY;
       }
     }
-    // the running maximum is only raised when a score passes it by more than 2^8, the weights' factor only lowered when one would pass 2^15
-    float top[NT][2];
-    bool raise = false;
+    // Probabilities and weights.  The running maximum and c only change when a weight passes what fp16 holds; a row without a maximum has infinite ones.
+    uint32_t pk[PP][NT][2];                        // weights of rows 2 tq + {0, 1}, tokens gq and gq + 8
+    float sum[NT][2];
+    auto weights = [&] {
+      uint32_t most = 0;
 #pragma unroll
-    for (int y = 0; y < NT; ++y)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float weight = 0.f;                        // (fmaxf drops the NaN of a row without a maximum)
-        top[y][e] = -INFINITY;
+      for (int y = 0; y < NT; ++y) {
+        sum[y][0] = l[y][0];
+        sum[y][1] = l[y][1];
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
-          const float own = fmaxf(s[p][y][e], s[p][y][2 + e]);
-          top[y][e] = fmaxf(top[y][e], own);
-          weight = fmaxf(weight, ex2(own - m[y][e]) * fminf(vs[p] * wc[y][e], FLT_MOST));
+          const float p0 = ex2(s[p][y][0] - m[y][0]), p1 = ex2(s[p][y][1] - m[y][1]), p2 = ex2(s[p][y][2] - m[y][0]), p3 = ex2(s[p][y][3] - m[y][1]);
+          const float v0 = fminf(vs[p] * wc[y][0], KV8_MOST_V), v1 = fminf(vs[p] * wc[y][1], KV8_MOST_V);        // (finite: a probability of zero stays one)
+          sum[y][0] += p0 + p2;
+          sum[y][1] += p1 + p3;
+          pk[p][y][0] = pack_f16(p0 * v0, p1 * v1);
+          pk[p][y][1] = pack_f16(p2 * v0, p3 * v1);
+          most = __vmaxu2(most, __vmaxu2(pk[p][y][0], pk[p][y][1]));
         }
-        raise |= top[y][e] > m[y][e] + 8.f || weight > 32768.f;
       }
-    if (__any_sync(0xffffffffu, raise)) {
+      return ((most + 0x04000400u) & 0x80008000u) != 0u;           // an infinity or NaN among them
+    };
+    if (__any_sync(0xffffffffu, weights())) {
 #pragma unroll
       for (int y = 0; y < NT; ++y)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
+          float top[PP], to = m[y][e], weight = 0.f;
 #pragma unroll
-          for (int x = 4; x < 32; x <<= 1) top[y][e] = fmaxf(top[y][e], __shfl_xor_sync(0xffffffffu, top[y][e], x));
-          const float to = fmaxf(m[y][e], top[y][e]), lift = to - m[y][e];
-          float weight = 0.f;
+          for (int p = 0; p < PP; ++p) {
+            top[p] = fmaxf(s[p][y][e], s[p][y][2 + e]);
 #pragma unroll
-          for (int p = 0; p < PP; ++p) weight = fmaxf(weight, ex2(fmaxf(s[p][y][e], s[p][y][2 + e]) - to) * vs[p]);
+            for (int x = 4; x < 32; x <<= 1) top[p] = fmaxf(top[p], __shfl_xor_sync(0xffffffffu, top[p], x));
+            to = fmaxf(to, top[p]);
+          }
 #pragma unroll
-          for (int x = 4; x < 32; x <<= 1) weight = fmaxf(weight, __shfl_xor_sync(0xffffffffu, weight, x));
+          for (int p = 0; p < PP; ++p) weight = fmaxf(weight, ex2(top[p] - to) * vs[p]);
           // c times the largest weight of the step to [2^6, 2^7), unless an earlier one is larger
-          const float was = (float)((int)(__float_as_uint(wc[y][e]) >> 23) - 127);
+          const bool first = m[y][e] == KV8_NONE;
+          const float lift = to - m[y][e], was = first ? (float)KV8_MOST_UP : (float)((int)(__float_as_uint(wc[y][e]) >> 23) - 127);
           const float now = fminf(fminf(was + floorf(lift), (float)(6 + 127 - (int)(__float_as_uint(weight) >> 23))), (float)KV8_MOST_UP);
-          if (to > m[y][e] || now < was) {
+          if (to > m[y][e] || (!first && now < was)) {
             const float f = ex2(now - was - lift);
             m[y][e] = to;
             l[y][e] *= ex2(-lift);
@@ -428,21 +438,16 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
             for (int j = 0; j < MT; ++j) { o[y][j][e] *= f; o[y][j][2 + e] *= f; }
           }
         }
+      weights();
     }
+#pragma unroll
+    for (int y = 0; y < NT; ++y) { l[y][0] = sum[y][0]; l[y][1] = sum[y][1]; }
 #pragma unroll
     for (int p = 0; p < PP; ++p) {
       const uint32_t vt = tiles + p * 2 * TILE + TILE;
       uint32_t pt[NT][2];                          // P^T as the B operand
 #pragma unroll
-      for (int y = 0; y < NT; ++y) {
-        const float m0 = m[y][0] == -INFINITY ? 0.f : m[y][0], m1 = m[y][1] == -INFINITY ? 0.f : m[y][1];
-        const float p0 = ex2(s[p][y][0] - m0), p1 = ex2(s[p][y][1] - m1), p2 = ex2(s[p][y][2] - m0), p3 = ex2(s[p][y][3] - m1);
-        l[y][0] += p0 + p2;
-        l[y][1] += p1 + p3;
-        const float v0 = fminf(vs[p] * wc[y][0], FLT_MOST), v1 = fminf(vs[p] * wc[y][1], FLT_MOST);        // (finite: a probability of zero stays one)
-        pt[y][0] = transpose_8x8(pack_f16(p0 * v0, p1 * v1));
-        pt[y][1] = transpose_8x8(pack_f16(p2 * v0, p3 * v1));
-      }
+      for (int y = 0; y < NT; ++y) { pt[y][0] = transpose_8x8(pk[p][y][0]); pt[y][1] = transpose_8x8(pk[p][y][1]); }
       // V^T as the A operand: bytes of two tokens interleaved, then two codes at a time to fp16; k indices 2 tq + {0, 1} and + 8 are
       // those tokens, rows gq and gq + 8 of m tile j the dims gq HD / 8 + 2 j + {0, 1}
       uint32_t w[4][HD / 32];
@@ -531,7 +536,7 @@ __global__ void __launch_bounds__(KV8_WARPS * 32, Kv8Geo<HD, NT>::BLOCKS) kv8_at
     for (int e = 0; e < 2; ++e) {
       const int r = 8 * y + 2 * tq + e;
       const float back = __int_as_float(0x7f000000 - __float_as_int(wc[y][e]));              // 1 / c
-      if (gq == 0) { sm_m[warp][r] = m[y][e]; sm_l[warp][r] = l[y][e]; }
+      if (gq == 0) { sm_m[warp][r] = m[y][e] == KV8_NONE ? -INFINITY : m[y][e]; sm_l[warp][r] = l[y][e]; }
 #pragma unroll
       for (int j = 0; j < MT; ++j)
         *reinterpret_cast<float2*>(sm_o + (warp * TR + r) * HD + gq * (HD / 8) + 2 * j) = make_float2(o[y][j][e] * back, o[y][j][2 + e] * back);
@@ -769,7 +774,7 @@ AttnPlan attn_plan(int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len
   }
   const int tile = p.nt ? 8 * p.nt : KV8_FLASH_ROWS;
   p.tiles = (int)((rows + tile - 1) / tile);
-  auto few = [&](int nt, long long tiles) { return kv8_chunks(B, (long long)B * tiles * Hkv, (nt == 1 ? 4 : 3) * sm_count, max_len); };
+  auto few = [&](int nt, long long tiles) { return kv8_chunks(B, (long long)B * tiles * Hkv, kv8_blocks(hd, nt) * sm_count, max_len); };
   if (p.nt) {
     const Chunks c = few(p.nt, p.tiles);
     p.chunk = c.tokens;

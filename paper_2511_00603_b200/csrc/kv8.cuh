@@ -7,6 +7,8 @@
 namespace epara {
 
 constexpr float KV8_TINY_SCALE = 1.17549435e-38f;     // 2^-126
+constexpr float KV8_MOST_V = 1.7014118e38f;           // 2^127: of a V scale times that factor
+constexpr float KV8_NONE = -3.4028234e38f;            // the maximum of a row that has seen no score
 constexpr int KV8_MOST_UP = 120;                      // weights -- probability x V scale -- are multiplied by at most 2^120 to make fp16 of them
 
 // two fp32 -> two e4m3 codes (lo in the low byte), nearest even, NaN to NaN
