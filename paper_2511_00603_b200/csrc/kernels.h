@@ -151,11 +151,12 @@ struct Kv8Attn {
   int q_stride, table_stride, B, T, Hkv, G, max_q, max_len;
   int tiles;               // row tiles of a request with max_q new tokens
   int min_n, max_n;        // new tokens of the requests that this launch takes
+  int ordered;             // many rows: the requests are put in order, and those that this launch does not take left out
   int part_tokens;         // 0: partial results by the rows of q, else so many for each request
   int chunk, max_chunks;   // tokens of a chunk, chunks of the longest request
 };
 constexpr int KV8_FLASH_ROWS = 256;      // query rows of a CTA in the kernel for many rows (kv8_flash.cu)
-constexpr int KV8_FLASH_SORTED = 1024;   // requests of a call that it puts in order
+constexpr int KV8_FLASH_SORTED = 1024, KV8_FLASH_MOST = 4096;   // requests of a call that it always puts in order, and at most
 cudaError_t launch_kv8_flash(const Kv8Attn& a, int hd, long long items, cudaStream_t st);       // items: row tiles of all requests, at least
 
 }  // namespace epara

@@ -738,6 +738,7 @@ int kv8_flash_chunk(long long requests, int tiles, int Hkv, int max_len, int sm_
 struct AttnPlan {
   int nt, tiles, chunk, chunks, clustered;           // nt 0: the kernel for many rows
   int few_tokens, few_nt, few_tiles, few_chunk, few_chunks, few_clustered;         // few_tokens 0: not split
+  int ordered;                                       // see Kv8Attn
   long long many_items;                              // row tiles of the kernel for many rows
 };
 // Which kernel: up to 16 query rows of a (request, kv head) the one for few rows, with tiles of 8 or 16; beyond them the one whose time is
@@ -791,9 +792,13 @@ AttnPlan attn_plan(int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len
       p.few_clustered = c.clustered;
       p.few_chunks = (max_len + p.few_chunk - 1) / p.few_chunk;
     }
-    // every request adds at most one tile to those that the rows fill
+    // Every request adds at most one tile to those that the rows fill.  To find a CTA its tile among more requests than KV8_FLASH_SORTED takes longer than it
+    // gains, but where the requests are not alike.  (1100 single tokens beside 512 of another request 606 us out of order, 129 in order; 2000 of 64 tokens
+    // 1720 and 2190.)
+    const long long fill = (long long)T * G / KV8_FLASH_ROWS + std::max(std::min(B, T / (p.few_tokens + 1)), 1);
     p.many_items = (long long)B * p.tiles;
-    if (B <= KV8_FLASH_SORTED) p.many_items = std::min(p.many_items, (long long)T * G / KV8_FLASH_ROWS + std::max(std::min(B, T / (p.few_tokens + 1)), 1));
+    p.ordered = B <= KV8_FLASH_SORTED || (B <= KV8_FLASH_MOST && 2 * fill < p.many_items);
+    if (p.ordered) p.many_items = std::min(p.many_items, fill);
   }
   p.chunks = (max_len + p.chunk - 1) / p.chunk;
   return p;
@@ -862,7 +867,7 @@ cudaError_t launch_few(const Kv8Attn& a, int nt, bool clustered, cudaStream_t st
 template <int HD>
 cudaError_t launch_attn(Kv8Attn a, const AttnPlan& p, cudaStream_t st) {
   a.tiles = p.tiles; a.chunk = p.chunk; a.max_chunks = p.chunks;
-  a.min_n = 1; a.max_n = a.max_q; a.part_tokens = 0;
+  a.min_n = 1; a.max_n = a.max_q; a.part_tokens = 0; a.ordered = p.ordered;
   if (p.nt) return launch_few<HD>(a, p.nt, p.clustered, st);
   if (p.few_tokens) {
     Kv8Attn f = a;

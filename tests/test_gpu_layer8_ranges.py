@@ -4,8 +4,8 @@ import math
 import pytest
 import torch
 
-from .test_gpu_layer8 import (F64, HALF_BF16, HALF_F16, HALF_F32, Cache, _append_reference, _attend, _check_norm, _gen, _int, _rows, _st, _status,
-                              _within)
+from .test_gpu_layer8 import (F64, HALF_BF16, HALF_F16, HALF_F32, Cache, Part, _append_reference, _attend, _check_attention, _check_norm, _gen, _int, _rows, _st,
+                              _status, _within)
 
 pytestmark = pytest.mark.gpu
 
@@ -168,6 +168,27 @@ def test_equal_scores_have_equal_weights(E, hd, power, n, max_len):
         # (a weight is exact but for its rounding to fp16 and the sum's roundings)
         tol = (HALF_F16 + 2.0 ** -16) * spread + HALF_BF16 * (mean.abs() + HALF_F16 * spread)
         assert ((out[i].to(F64).view(4, hd) - mean).abs() <= tol).all(), i
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("B", [48, 49, 700, 4096, 4200])
+def test_many_requests_with_several_tokens_each(E, hd, B):
+    """Some hundreds or thousands of requests for the kernel for many rows, many of one length, some without rows: each row is computed, and once."""
+    G, Hkv = 8, 1
+    ns = [(5 + 7 * i) % 41 if i % 3 else 0 for i in range(B)]
+    ns[B // 2], ns[B - 1] = 200, 33
+    lens = [n + (13 * i) % 50 if i % 4 else 150 + n // 2 for i, n in enumerate(ns)]
+    c = Cache(B, 1 << 20, Hkv, hd, B, used=max(lens))
+    T = sum(ns)
+    q = torch.randn((T + 2, G * hd), generator=_gen(B), device="cuda").to(torch.bfloat16)
+    out, st = _attend(E, c, q, lens, ns, G)
+    assert st.item() == 0 and (out[T:] == 55).all()
+    starts = _rows(ns)[1]
+    for b in sorted({0, 1, 2, 4, B // 2, B - 2, B - 1, *range(5, B, max(1, B // 40))}):
+        if ns[b]:
+            _check_attention(Part(c, b), q, [lens[b]], [ns[b]], G, out, f"request {b}", row0=starts[b])
+    one, _ = _attend(E, c, q, lens, ns, G, max_len=max(lens))           # (fewer tokens at most: other kernels, other chunks)
+    assert torch.equal(torch.isfinite(one.float()), torch.isfinite(out.float())) and ((one.float() - out.float()).abs() <= 0.05 * out.float().abs().amax(1, keepdim=True)).all()
 
 
 # ------------------------------------------------------------------------------------------------ append
