@@ -8,8 +8,9 @@
 //   pair    256-row tiles on pairs of CTAs, persistent, two accumulators.
 // (A third one for up to 16 rows on mma.sync, as for bf16, was slower here: 1 x 32000 x 4096 35 us, swapped operands 23;
 // 16 x 6144 x 4096 11.4 and 8.8; 1 x 6144 x 4096 9.0 and 8.5.)
-// Few rows are bound by HBM or, below 30 MB of W, by the latencies of a launch and a first tile: 1 x 6144 x 4096 6.8 us (floor 3.8), 96 x 28672 x
-// 4096 27 us, 4.4 TB/s (18.4).  Many by the tensor cores: 8192 x 4096 x 14336 332 us, 2900 TOP/s, 87 % of twice what cuBLAS does in bf16.
+// Few rows are bound by HBM or, below 30 MB of W, by the latencies of a launch and a first tile: 1 x 6144 x 4096 8.5 us with W cold, 6.6 with
+// W in L2 (floor 3.8), 96 x 28672 x 4096 27 us, 4.4 TB/s (18.4).  Many by the tensor cores: 8192 x 4096 x 14336 332 us at the full clock, 2900 TOP/s, 87 % of twice what
+// cuBLAS does in bf16; 390 in calls that keep the GPU at its power limit, where the clock falls from 1965 to 1290 MHz (on zeros 263).
 // Operands come by plain TMA (columns past K and rows past the matrix arrive as zeros), products run as tcgen05.mma kind::i8,
 // sums are in tensor memory.  Every wait is bounded; a kernel that gives up leaves a code in *status.
 #include <algorithm>

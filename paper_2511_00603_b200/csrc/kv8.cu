@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(APPEND_WARPS * 32) kv8_append_kernel(const Kv8
 // row's largest weight still is a normal fp16, and what a row does not see, or gives no weight, takes no bits from it.  (Relative to the largest V scale
 // instead, a page whose V is 2^26 times the others' took all of theirs.)  Which dim a k index of the first product stands for, and which one a row of the
 // second, is free, and is chosen so that a lane reads 16 consecutive bytes of K and of V.
-// Bound by HBM: 128 requests of 512 to 8192 tokens, 8 kv heads, G 4, hd 128 190 us, 6.0 TB/s (floor 175); two of 100003 and 131072 90 us,
+// Bound by HBM: 128 requests of 512 to 8192 tokens, 8 kv heads, G 4, hd 128 189 us, 6.0 TB/s (floor 175); two of 100003 and 131072 89 us,
 // 5.3 TB/s (72), one round of 536 blocks and the merge; one of a few hundred tokens 6 us, latencies.  On the tensor cores since the
 // first form, on FMAs, took 278 us for the first of these: a code and its product are three instructions there.
 __device__ __forceinline__ uint2 lds8(uint32_t a) {
@@ -188,7 +188,7 @@ constexpr int kv8_blocks(int hd, int nt) { return nt == 1 ? 4 : hd == 64 ? 3 : 2
 template <int HD, int NT>
 struct Kv8Geo {
   // pages that a warp takes at once (hd 64: what a step costs beside its products is paid for two), steps in its ring, blocks to an SM: for 16 rows of hd 128
-  // two, for in the registers of three the loop spills (32 requests of 4096 with 4 tokens each 69 us, three 95; hd 64 three 49, two 49, 64 requests with 8 tokens
+  // two, for in the registers of three the loop spills (32 requests of 4096 with 4 tokens each 58 us, three 95; hd 64 three 49, two 49, 64 requests with 8 tokens
   // 128 and 157)
   static constexpr int PAGES = HD == 64 ? 2 : 1, STAGES = NT == 1 ? 3 : 4, BLOCKS = kv8_blocks(HD, NT);
   static constexpr int RING = KV8_WARPS * STAGES * PAGES * 2 * PAGE * HD, MERGE = KV8_WARPS * 8 * NT * HD * 4;
@@ -743,7 +743,7 @@ struct AttnPlan {
 };
 // Which kernel: up to 16 query rows of a (request, kv head) the one for few rows, with tiles of 8 or 16; beyond them the one whose time is
 // estimated to be the shortest.  The figures, in microseconds, were fitted to all three on 850 shapes of 12 to 2048 rows, 1 to 64 requests and 128 to
-// 65536 tokens: what is chosen takes 1.2 % longer than the best on average, the estimates are off by 14 %.  The kernel for few rows pays for tiles and for a tile's tokens,
+// 65536 tokens: what was chosen took 1.2 % longer than the best on average, with the kernels as they are now 1.6 %, the estimates being off by 11 %.  The kernel for few rows pays for tiles and for a tile's tokens,
 // the one for many for rounds of its CTAs, their steps and, with several chunks, the partial results.
 double few_us(int hd, int nt, double items, double tokens) {
   return hd == 128 ? (nt == 1 ? 7.2 + 0.0064 * items + 3.3e-5 * items * tokens : 10.7 + 0.0136 * items + 5.2e-5 * items * tokens)

@@ -10,22 +10,22 @@
 // page.  Roles:
 //   warps 0-3, 4-7  softmax of tile 0 and 1, one thread per query row (at first: that row of Q into shared memory).  A row of S is read
 //                   from tensor memory once and P written over it in fp16.  The running maximum is raised, and O rescaled, only when
-//                   it grows by more than 2^8.  The warps of the two tiles on a scheduler take turns at the exponentials, so that one tile's
+//                   it grows by more than 2^8 or a weight would pass 2^15.  The warps of the two tiles on a scheduler take turns at the exponentials, so that one tile's
 //                   scores are read and reduced while the other keeps the special-function unit busy;
 //   warps 8, 9      issue S_g = Q_g K^T (M 128, N 64) into one of two buffers per tile, g = 0 and 1;
 //   warps 10, 11    issue O_g += P_g V, P as the A operand from tensor memory, V as an MN-major B operand;
-//   warps 12-15     request the pages of the next steps, one of each, and write them as the 128-byte-swizzled tiles that the MMAs want.  NaN
+//   warps 12-15     request the pages of the next steps, one of each, and write them as the 128-byte-swizzled tiles that the MMAs want, and their scales where the softmax warps read them.  NaN
 //                   codes of V are taken out (a zero probability times NaN is NaN) and the first key that has one is kept per dim: a row that
 //                   sees it gets its NaN at the end.
 // With several chunks of keys partial results go to scratch, as in the kernel for few rows, and are merged by the same kernel.
 // Every mbarrier wait is bounded.
 //
 // Bound by the tensor cores on paper (2 products of rows x keys x hd), in fact by no unit alone.  Four prompt chunks of 509 to 1024 new tokens
-// after up to 8192, 32 heads over 8, hd 128: 271 us, 877 TFLOP/s; hd 64: 216.  A step takes 2250 cycles: the tensor cores are at work in 1280
+// after up to 8192, 32 heads over 8, hd 128: 266 us, 893 TFLOP/s; hd 64: 213.  A step takes 2200 cycles: the tensor cores are at work in 1280
 // (an MMA of N 64 takes 3/4 of one of N 128, as all of Q is read for it), the special-function unit in 1024, shared memory, by its bytes, in
-// 1500.  Without any exponentials it would take 5 % less, without the conversion 4 %, with an eighth of Q K^T 4.5 %.  9 us of a CTA are not its
+// 1500.  Without any exponentials it took 5 % less, without the conversion 4 %, with an eighth of Q K^T 4.5 %.  9 us of a CTA are not its
 // loop, and the last round of CTAs leaves 7 % of the SMs idle.  Tried: 16 softmax warps, two threads to a row, 295; 128 keys to a pass of the softmax, 295 (a longer chain from P V to
-// the next scores outweighs the fewer hand-overs); without turns 283; the page scales of a step fetched in the one before 267, but 219 for hd 64.
+// the next scores outweighs the fewer hand-overs); without turns 283 (against 271 then).
 #include <climits>
 
 #include "../../include/epara.h"
