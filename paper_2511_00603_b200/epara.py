@@ -536,9 +536,7 @@ def _cache(kv8_layer, kv_scales, kv_lens, tables, q_rows, status, pages, B, Hkv,
     if one != 1 or n < B or tables.dtype is not _I32 or tables.get_device() != at:
         _matrix("tables", tables, B, width, _I32, at)
     if q_rows is not None:
-        if q_rows.numel() != B + 1:
-            raise ValueError("q_rows has one element more than there are requests")
-        if q_rows.dtype is not _I32 or q_rows.get_device() != at or not q_rows.is_contiguous():
+        if q_rows.dtype is not _I32 or q_rows.get_device() != at or q_rows.numel() <= B or not q_rows.is_contiguous():
             _vector("q_rows", q_rows, B + 1, _I32, at)
     if status.dtype is not _I32 or status.get_device() != at:
         _wants("status", status, _I32, at)

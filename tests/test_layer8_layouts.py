@@ -115,7 +115,7 @@ def test_product_wants_an_fp32_stream_and_half_the_columns_of_a_gated_one(E):
 
 POOL = torch.zeros((9, 3, 2, 2, 16, 64), dtype=torch.float8_e4m3fn)
 CACHE_LAYOUTS = [("layer", POOL[:, 1]), ("scales", torch.zeros((9, 3, 2, 2))[:, 1]), ("scales", torch.zeros((8, 2, 2))), ("lens", torch.ones(6, dtype=i32)[::2]),
-                 ("tables", _wide(3, 4, i32)), ("tables", torch.zeros((2, 4), dtype=i32)), ("q_rows", torch.zeros(3, dtype=i32)), ("q_rows", torch.zeros(5, dtype=i32)),
+                 ("tables", _wide(3, 4, i32)), ("tables", torch.zeros((2, 4), dtype=i32)), ("q_rows", torch.zeros(3, dtype=i32)),
                  ("q_rows", torch.zeros(8, dtype=i32)[::2]), ("kv_pages", 10)]
 CACHE_TYPES = [("layer", POOL[:, 1].to(torch.float16).contiguous()), ("scales", torch.zeros((9, 2, 2), dtype=bf)), ("lens", torch.ones(3, dtype=torch.int64)),
                ("tables", torch.zeros((3, 4), dtype=torch.int64)), ("q_rows", torch.arange(4)), ("status", torch.zeros(1, dtype=torch.int64))]
@@ -180,6 +180,9 @@ def test_what_arrives(E):
     assert a[3] == a[5] == 128 and a[8] == 5 and a[9] is None and a[12] == 4
     a = _attend(E, q=qkv.view(3, 512)[:, :256], tables=torch.zeros((3, 7), dtype=i32)[:, :4], scratch=torch.zeros(80, dtype=torch.uint8))
     assert a[3] == 512 and a[10] == 7 and a[20] == 80
+    buffers = dict(q_rows=torch.zeros(9, dtype=i32), tables=torch.zeros((8, 4), dtype=i32), out=torch.zeros((8, 256), dtype=bf))           # larger than the call needs
+    assert _attend(E, **buffers)[12] == 3
+    assert _norm(E, q=torch.zeros((9, 72), dtype=i8), scales=torch.zeros(9), resid=torch.zeros((5, 64)))[12] == 72
     assert _attend(E, q=qkv[:, :4])[3] == 512 and _attend(E, out=torch.zeros((3, 4, 64), dtype=bf))
     assert _attend(E, layer=torch.zeros((9, 2, 2, 16, 64), dtype=torch.uint8))
 
