@@ -793,7 +793,7 @@ AttnPlan attn_plan(int B, int T, int Hq, int Hkv, int hd, int max_q, int max_len
       p.few_chunks = (max_len + p.few_chunk - 1) / p.few_chunk;
     }
     // Every request adds at most one tile to those that the rows fill.  To find a CTA its tile among more requests than KV8_FLASH_SORTED takes longer than it
-    // gains, but where the requests are not alike.  (1100 single tokens beside 512 of another request 606 us out of order, 129 in order; 2000 of 64 tokens
+    // gains, but where the requests are not alike.  (1100 single tokens beside 512 of another request 606 us out of order, 121 in order; 2000 of 64 tokens
     // 1720 and 2190.)
     const long long fill = (long long)T * G / KV8_FLASH_ROWS + std::max(std::min(B, T / (p.few_tokens + 1)), 1);
     p.many_items = (long long)B * p.tiles;
